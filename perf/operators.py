@@ -272,7 +272,9 @@ def _plain_append(c, k, v, places, past, new):
     c["scales"][:, ids] = scale.view(2, seqs * blocks, -1)
     open_at = ((held + new) // PAGE * PAGE)[:, None] + torch.arange(PAGE, device="cuda")
     seq = torch.arange(seqs, device="cuda")[:, None]
-    c["tail"].copy_(rows[:, seq, open_at.clamp(max=blocks * PAGE - 1)])
+    # (a block that was filled leaves the tail as it was: the pass can be made again)
+    left = ((held + new) % PAGE > 0)[None, :, None, None, None]
+    c["tail"].copy_(torch.where(left, rows[:, seq, open_at.clamp(max=blocks * PAGE - 1)], c["tail"]))
 
 
 def _plain_held(c):
