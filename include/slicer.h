@@ -292,6 +292,97 @@ int slicer_check(const void* meta, uint64_t stream_words, slicer_dtype dt, int64
 int slicer_stream_words(const void* meta, uint64_t* words, void* hip_stream);
 
 /*
+ * The attention cache in 8 bits.  In auto-regressive inference (Sec. 2.1: the front end runs w - 1 steps by itself under a memory budget before it
+ * offloads step w) either side holds the keys and values of the tokens that its layers have seen: the one intermediate feature that is held instead of
+ * sent.  These calls hold it in 8 bits with a scale for each block of 64 tokens and head, attend over it, shrink it by the attention that its
+ * blocks have received, and read it back (for slicer_encode, where it is handed over after all).
+ *
+ *   page     64 tokens of one sequence, in every head.  A sequence's i-th page is page_table[sequence][i]; pages of one sequence may stand
+ *            anywhere and full pages may be shared by sequences (a common prefix).  Tokens are rounded to bf16 (nearest even) as they come; those of the page
+ *            that is not full yet are held so, in the sequence's tail.  When a page gets full its 64 x head_dim keys of a head are held as
+ *            code * scale, with amax their largest magnitude: scale = amax / 127, code = rint(x * (127 / amax)) within -127..127, every step one fp32
+ *            operation; values likewise, with a scale of their own.  amax < 2^-119: zeros.  The result does not depend on how many tokens a call brings.
+ *   values   finite, magnitudes up to 2^100.  A token with others is held as a key of NaN and a value of zero, in a full page as zeros under a key scale of
+ *            NaN: outputs of queries that see it (in a full page: that see the page) are NaN, no others are touched.
+ *   handle   slicer_kv is read on the host during a call; its pointers are device memory of the caller, 256-byte aligned, sizes from slicer_kv_sizes.
+ *            pages, scales and tails need no initial values.  page_table and lens are the caller's to keep, on the device; entries that
+ *            lie outside the cache are never followed: a page_table entry outside [0, n_pages) is not written, and read as NaN; lens are taken as
+ *            if within [0, 64 max_pages], starts as if within [0, tokens].
+ *   batches  a call's new tokens (queries) of sequence i are rows starts[i] .. starts[i + 1] - 1 of [tokens][heads][head_dim] tensors (device array, seqs + 1
+ *            entries); a sequence may have none.  Rows outside every sequence are left as they were.  lens[i] counts the sequence's tokens with the call's new ones.
+ *            max_new: no sequence has more new tokens (those of a longer one are left out).
+ * dt is the type of k, v, q and out; softmax, sums and weights are fp32.  All calls but slicer_kv_sizes and slicer_kv_attend_sizes, which are host
+ * computations, are asynchronous on hip_stream, allocate nothing and can be captured into a HIP graph.  Calls that share a workspace, or of
+ * which one writes what another reads, must be ordered by the caller; others may overlap.
+ * Errors: SLICER_EINVAL for null pointers, seqs, heads, max_pages or n_pages < 1 (max_pages > 2^24, n_pages >= 2^31, seqs * kv_heads >= 2^22),
+ * head_dim no multiple of 8 in 8..256, max_new < 1 with tokens > 0, negative tokens, and what the calls name; SLICER_EUNSUPPORTED for an unknown dtype.
+ */
+#define SLICER_KV_PAGE 64
+
+typedef struct slicer_kv {
+    void* pages;                 /* codes */
+    float* scales;               /* [n_pages][kv_heads][2]: of the keys, of the values */
+    void* tails;                 /* the tokens of the pages that are not full */
+    const int32_t* page_table;   /* [seqs][max_pages] */
+    const int32_t* lens;         /* [seqs] */
+    int32_t seqs, kv_heads, head_dim, max_pages;
+    int64_t n_pages;
+} slicer_kv;
+
+/* Bytes of the three buffers: pages n_pages * kv_heads * 128 * dp, scales n_pages * kv_heads * 8, tails seqs * kv_heads * 256 * dp, with dp =
+ * head_dim rounded up to 32.  Pointers in kv are not looked at; output pointers may be NULL. */
+int slicer_kv_sizes(const slicer_kv* kv, size_t* pages_bytes, size_t* scales_bytes, size_t* tails_bytes);
+
+/*
+ * Takes new tokens into the cache: places lens[i] - new .. lens[i] - 1 of sequence i.
+ *   k, v       [tokens][kv_heads][head_dim], element stride 1; k_token, k_head, v_token, v_head: strides of tokens and heads in elements
+ * A call can be made again with the same arguments as long as it did not fill a page and begin another from tokens of before and of the call.
+ */
+int slicer_kv_append(const slicer_kv* kv, const void* k, const void* v, slicer_dtype dt, int64_t tokens, const int32_t* starts, int max_new,
+                     int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* hip_stream);
+
+/*
+ * Attention over the cache.  Query i of a sequence's n, head h, with kv head h / (heads / kv_heads), sees the tokens 0 .. lens - n + i (causal: the
+ * query's own token is the last one it sees) or all lens tokens; out = sum softmax(scale * q . key) value.  A query that sees none gets zeros.
+ *   q          [tokens][heads][head_dim], element stride 1, strides q_token, q_head in elements
+ *   heads      a multiple of kv_heads
+ *   out        [tokens][heads][head_dim], contiguous; may not overlap q
+ *   lse        [tokens][heads] fp32 or NULL: log of the sum of exp(scale * q . key); -inf for a query that sees nothing
+ *   mass       [seqs][kv_heads][max_pages] fp32 or NULL: mass = mass_decay * mass + the sum of the probabilities that the page's tokens got from the
+ *              call's queries in the kv head's query heads, for the pages that hold tokens of sequences with new ones; others stay.  mass_decay in [0, 1]; with 0
+ *              the old contents are not read.
+ *   workspace  slicer_kv_attend_sizes bytes, 256-byte aligned; contents undefined before and after
+ *   max_len    what lens are expected to stay within; it decides how the work is split, never the result's validity
+ * The result is a function of the arguments alone: nothing is summed in an order that changes from call to call.
+ * Errors: SLICER_EINVAL for heads no multiple of kv_heads, scale not finite, mass_decay outside [0, 1], max_len < 0.
+ */
+int slicer_kv_attend_sizes(const slicer_kv* kv, int heads, int64_t tokens, int max_new, int64_t max_len, size_t* workspace_bytes);
+int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int heads, int64_t tokens, const int32_t* starts, int max_new,
+                     int64_t max_len, int64_t q_token, int64_t q_head, double scale, int causal, void* out, float* lse, float* mass, double mass_decay,
+                     void* workspace, void* hip_stream);
+
+/*
+ * Reads the cache back: rows starts[i] .. of k and v ([tokens][kv_heads][head_dim], contiguous) get tokens 0, 1, ... of sequence i, as code * scale in fp32 or
+ * the tail's bf16, rounded to dt; rows beyond lens[i] stay.  max_new as above.
+ */
+int slicer_kv_read(const slicer_kv* kv, void* k, void* v, slicer_dtype dt, int64_t tokens, const int32_t* starts, int max_new, void* hip_stream);
+
+/*
+ * Drops the full pages that have received the least attention, in every sequence that has more than keep_pages of them: the first sink_pages, the last
+ * recent_pages and the heaviest of the others stay, keep_pages in all.  A page's weight is the sum of mass over the kv heads, in fp64; equal weights: the
+ * lower place stays (the rule of slicer_encode's top-K); NaN counts as largest.  Later pages move up in page_table and mass, the page that is not full and entries behind it too;
+ * no codes move, and slots left over hold -1 and 0.  A later query sees the tokens that are left as its predecessors.
+ *   mass          [seqs][kv_heads][max_pages]
+ *   page_table_out, lens_out, mass_out   as kv->page_table, kv->lens and mass, or those very arrays (no other overlap)
+ *   freed         [seqs][max_pages]: the dropped pages in their order, then -1; n_freed [seqs]: how many
+ *   workspace     8 * seqs * max_pages bytes, 256-byte aligned
+ * pages, scales and tails of the handle are not looked at and may be NULL.
+ * Errors: SLICER_EINVAL for negative counts or sink_pages + recent_pages > keep_pages.
+ */
+int slicer_kv_evict(const slicer_kv* kv, const float* mass, int keep_pages, int sink_pages, int recent_pages, int32_t* page_table_out, int32_t* lens_out,
+                    float* mass_out, int32_t* freed, int32_t* n_freed, void* workspace, void* hip_stream);
+
+/*
  * Timing hook for benchmarks.  While both events are non-NULL (hipEvent_t cast to
  * void*), every slicer_encode / slicer_decode / slicer_decode_as issued by the
  * calling thread records `start` immediately before and `stop` immediately after

@@ -19,6 +19,14 @@ _TORCH_DT = {torch.float32: SLICER_F32, torch.bfloat16: SLICER_BF16}
 
 _lib = None
 
+SLICER_KV_PAGE = 64
+
+
+class SlicerKv(C.Structure):
+    """struct slicer_kv of include/slicer.h."""
+    _fields_ = [("pages", C.c_void_p), ("scales", C.c_void_p), ("tails", C.c_void_p), ("page_table", C.c_void_p), ("lens", C.c_void_p),
+                ("seqs", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int64)]
+
 
 class SlicerError(RuntimeError):
     def __init__(self, fn: str, code: int):
@@ -82,6 +90,19 @@ def load() -> C.CDLL:
         L.slicer_stream_words.argtypes = [vp, C.POINTER(C.c_uint64), vp]
         L.slicer_arith_probe.restype = cint
         L.slicer_arith_probe.argtypes = [cint, vp, vp, vp, i64, vp]
+        kvp = C.POINTER(SlicerKv)
+        L.slicer_kv_sizes.restype = cint
+        L.slicer_kv_sizes.argtypes = [kvp, szp, szp, szp]
+        L.slicer_kv_append.restype = cint
+        L.slicer_kv_append.argtypes = [kvp, vp, vp, cint, i64, vp, cint, i64, i64, i64, i64, vp]
+        L.slicer_kv_attend_sizes.restype = cint
+        L.slicer_kv_attend_sizes.argtypes = [kvp, cint, i64, cint, i64, szp]
+        L.slicer_kv_attend.restype = cint
+        L.slicer_kv_attend.argtypes = [kvp, vp, cint, cint, i64, vp, cint, i64, i64, i64, dbl, cint, vp, vp, vp, dbl, vp, vp]
+        L.slicer_kv_read.restype = cint
+        L.slicer_kv_read.argtypes = [kvp, vp, vp, cint, i64, vp, cint, vp]
+        L.slicer_kv_evict.restype = cint
+        L.slicer_kv_evict.argtypes = [kvp, vp, cint, cint, cint, vp, vp, vp, vp, vp, vp, vp]
         L.slicer_profile_events.restype = cint
         L.slicer_profile_events.argtypes = [vp, vp]
         L.slicer_last_hip_error.restype = cint
@@ -328,3 +349,168 @@ def slicer_arith_probe(op: int, a: torch.Tensor, b: torch.Tensor, out: torch.Ten
 def slicer_profile_events(start_event, stop_event) -> None:
     """Raw hipEvent_t handles (ints) or None, None: see include/slicer.h."""
     _check("slicer_profile_events", load().slicer_profile_events(start_event, stop_event))
+
+
+# ---- the attention cache in 8 bits ---------------------------------------------------------------------------------------
+
+
+class KvCache:
+    """The cache's buffers (see slicer_kv in include/slicer.h): page_table and lens are the program's to keep."""
+
+    def __init__(self, pages, scales, tails, page_table, lens, seqs, kv_heads, head_dim, n_pages, max_pages):
+        self.pages, self.scales, self.tails, self.page_table, self.lens = pages, scales, tails, page_table, lens
+        self.seqs, self.kv_heads, self.head_dim, self.n_pages, self.max_pages = seqs, kv_heads, head_dim, n_pages, max_pages
+        self._c, self._key = None, None
+
+    def c(self) -> SlicerKv:
+        """The C handle of the tensors as they are now."""
+        key = (self.pages.data_ptr(), self.scales.data_ptr(), self.tails.data_ptr(), self.page_table.data_ptr(), self.lens.data_ptr(),
+               self.seqs, self.kv_heads, self.head_dim, self.max_pages, self.n_pages)
+        if key != self._key:
+            _kv_tensor("page_table", self.page_table, torch.int32, (self.seqs, self.max_pages))
+            _kv_tensor("lens", self.lens, torch.int32, (self.seqs,))
+            sizes = _kv_sizes(SlicerKv(None, None, None, None, None, *key[5:]))
+            for name, t, size in zip(("pages", "scales", "tails"), (self.pages, self.scales, self.tails), sizes):
+                if not t.is_cuda or not t.is_contiguous() or t.numel() * t.element_size() < size:
+                    raise ValueError(f"{name} must be a contiguous tensor of {size} bytes on the GPU")
+            self._c, self._key = SlicerKv(*key), key
+        return self._c
+
+
+class KvEvicted:
+    """What slicer_kv_evict writes: the tables that follow, the pages that came free and how many, and its workspace."""
+
+    def __init__(self, page_table, lens, mass, freed, n_freed, workspace):
+        self.page_table, self.lens, self.mass, self.freed, self.n_freed, self.workspace = page_table, lens, mass, freed, n_freed, workspace
+
+
+def _kv_tensor(name: str, t: torch.Tensor, dtype, shape) -> None:
+    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on the GPU")
+
+
+def _kv_sizes(c: SlicerKv):
+    a, b, t = C.c_size_t(0), C.c_size_t(0), C.c_size_t(0)
+    _check("slicer_kv_sizes", load().slicer_kv_sizes(C.byref(c), C.byref(a), C.byref(b), C.byref(t)))
+    return a.value, b.value, t.value
+
+
+def slicer_kv_sizes(seqs: int, kv_heads: int, head_dim: int, n_pages: int, max_pages: int):
+    """(pages_bytes, scales_bytes, tails_bytes) of a cache."""
+    return _kv_sizes(SlicerKv(None, None, None, None, None, seqs, kv_heads, head_dim, max_pages, n_pages))
+
+
+def alloc_kv(seqs: int, kv_heads: int, head_dim: int, n_pages: int, max_pages: int, device="cuda") -> KvCache:
+    """A cache of n_pages pages of 64 tokens for seqs sequences of up to max_pages pages: all empty, no page handed out (-1)."""
+    pb, sb, tb = slicer_kv_sizes(seqs, kv_heads, head_dim, n_pages, max_pages)
+    return KvCache(torch.empty(pb, dtype=torch.uint8, device=device), torch.empty(sb // 4, dtype=torch.float32, device=device),
+                   torch.empty(tb // 2, dtype=torch.bfloat16, device=device),
+                   torch.full((seqs, max_pages), -1, dtype=torch.int32, device=device), torch.zeros(seqs, dtype=torch.int32, device=device),
+                   seqs, kv_heads, head_dim, n_pages, max_pages)
+
+
+def _kv_rows(name: str, x: torch.Tensor, heads: int, head_dim: int, device) -> None:
+    if not x.is_cuda or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim or x.device != device:
+        raise ValueError(f"{name} must be a [tokens, {heads}, {head_dim}] tensor on the cache's GPU")
+    if x.stride(2) != 1 and head_dim > 1:
+        raise ValueError(f"{name}: the elements of a head must lie next to each other")
+
+
+def _kv_call(kv: KvCache, starts: torch.Tensor):
+    c = kv.c()
+    _kv_tensor("starts", starts, torch.int32, (kv.seqs + 1,))
+    _kv_devices(kv, kv.scales, kv.tails, kv.page_table, kv.lens, starts)
+    return c
+
+
+def _kv_devices(kv: KvCache, *tensors) -> None:
+    """Kernels go to the current device: everything has to be there."""
+    here = torch._C._cuda_getDevice()
+    if kv.pages.device.index != here:
+        raise ValueError("the cache is not on the current device")
+    for t in tensors:
+        if t is not None and t.device != kv.pages.device:
+            raise ValueError("tensors of one call must be on one device")
+
+
+def slicer_kv_append(kv: KvCache, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, max_new: int, stream=None) -> None:
+    """Takes the tokens k, v [tokens, kv_heads, head_dim] into the cache; rows starts[i]..starts[i+1] are the last tokens of sequence i's lens[i]."""
+    c = _kv_call(kv, starts)
+    _kv_rows("k", k, kv.kv_heads, kv.head_dim, kv.pages.device)
+    _kv_rows("v", v, kv.kv_heads, kv.head_dim, kv.pages.device)
+    if k.shape[0] != v.shape[0] or k.dtype != v.dtype:
+        raise ValueError("k and v must have the same type and number of tokens")
+    _check("slicer_kv_append", load().slicer_kv_append(C.byref(c), k.data_ptr(), v.data_ptr(), _dt_of(k), k.shape[0], starts.data_ptr(), max_new,
+                                                       k.stride(0), k.stride(1), v.stride(0), v.stride(1), _stream_handle(stream)))
+
+
+def slicer_kv_attend_sizes(kv: KvCache, heads: int, tokens: int, max_new: int, max_len: int) -> int:
+    """Workspace bytes of slicer_kv_attend."""
+    w = C.c_size_t(0)
+    _check("slicer_kv_attend_sizes", load().slicer_kv_attend_sizes(C.byref(kv.c()), heads, tokens, max_new, max_len, C.byref(w)))
+    return w.value
+
+
+def alloc_kv_workspace(kv: KvCache, heads: int, tokens: int, max_new: int, max_len: int) -> torch.Tensor:
+    return torch.empty(max(slicer_kv_attend_sizes(kv, heads, tokens, max_new, max_len), 256), dtype=torch.uint8, device=kv.pages.device)
+
+
+def slicer_kv_attend(kv: KvCache, q: torch.Tensor, starts: torch.Tensor, max_new: int, max_len: int, scale: float, out: torch.Tensor,
+                     workspace: torch.Tensor, lse=None, mass=None, mass_decay: float = 0.0, causal: bool = True, stream=None) -> None:
+    """Attention of the queries q [tokens, heads, head_dim] over the cache, whose last tokens are theirs; workspace from alloc_kv_workspace with the
+    same numbers.  lse [tokens, heads] and mass [seqs, kv_heads, max_pages] (fp32) are optional outputs."""
+    c = _kv_call(kv, starts)
+    tokens, heads = q.shape[0], q.shape[1] if q.dim() == 3 else 0
+    _kv_rows("q", q, heads, kv.head_dim, kv.pages.device)
+    _kv_tensor("out", out, q.dtype, q.shape)
+    if lse is not None:
+        _kv_tensor("lse", lse, torch.float32, (tokens, heads))
+    if mass is not None:
+        _kv_tensor("mass", mass, torch.float32, (kv.seqs, kv.kv_heads, kv.max_pages))
+    L = load()
+    need = C.c_size_t(0)
+    _check("slicer_kv_attend_sizes", L.slicer_kv_attend_sizes(C.byref(c), heads, tokens, max_new, max_len, C.byref(need)))
+    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need.value:
+        raise ValueError(f"workspace must be a contiguous tensor of {need.value} bytes on the GPU")
+    _kv_devices(kv, out, lse, mass, workspace)
+    _check("slicer_kv_attend", L.slicer_kv_attend(
+        C.byref(c), q.data_ptr(), _dt_of(q), heads, tokens, starts.data_ptr(), max_new, max_len, q.stride(0), q.stride(1), scale, int(causal),
+        out.data_ptr(), lse.data_ptr() if lse is not None else None, mass.data_ptr() if mass is not None else None, mass_decay,
+        workspace.data_ptr(), _stream_handle(stream)))
+
+
+def slicer_kv_read(kv: KvCache, starts: torch.Tensor, max_new: int, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+    """Rows starts[i].. of k and v [tokens, kv_heads, head_dim] get the first tokens of sequence i."""
+    c = _kv_call(kv, starts)
+    _kv_tensor("k", k, k.dtype, (k.shape[0], kv.kv_heads, kv.head_dim))
+    _kv_tensor("v", v, k.dtype, k.shape)
+    _kv_devices(kv, k, v)
+    _check("slicer_kv_read", load().slicer_kv_read(C.byref(c), k.data_ptr(), v.data_ptr(), _dt_of(k), k.shape[0], starts.data_ptr(), max_new,
+                                                   _stream_handle(stream)))
+
+
+def alloc_kv_evict(kv: KvCache) -> KvEvicted:
+    dev = kv.pages.device
+    return KvEvicted(torch.empty_like(kv.page_table), torch.empty_like(kv.lens),
+                     torch.empty(kv.seqs, kv.kv_heads, kv.max_pages, dtype=torch.float32, device=dev),
+                     torch.empty_like(kv.page_table), torch.empty_like(kv.lens),
+                     torch.empty(8 * kv.seqs * kv.max_pages, dtype=torch.uint8, device=dev))
+
+
+def slicer_kv_evict(kv: KvCache, mass: torch.Tensor, keep_pages: int, sink_pages: int, recent_pages: int, out: KvEvicted, stream=None) -> None:
+    """Drops the full pages with the least mass where a sequence has more than keep_pages.  `out` gets the tables that follow (its page_table, lens and
+    mass may be the cache's and `mass` themselves)."""
+    c = kv.c()
+    table, by_head = (kv.seqs, kv.max_pages), (kv.seqs, kv.kv_heads, kv.max_pages)
+    _kv_tensor("mass", mass, torch.float32, by_head)
+    _kv_tensor("out.page_table", out.page_table, torch.int32, table)
+    _kv_tensor("out.lens", out.lens, torch.int32, (kv.seqs,))
+    _kv_tensor("out.mass", out.mass, torch.float32, by_head)
+    _kv_tensor("out.freed", out.freed, torch.int32, table)
+    _kv_tensor("out.n_freed", out.n_freed, torch.int32, (kv.seqs,))
+    if not out.workspace.is_cuda or not out.workspace.is_contiguous() or out.workspace.numel() * out.workspace.element_size() < 8 * kv.seqs * kv.max_pages:
+        raise ValueError("out.workspace is too small")
+    _kv_devices(kv, kv.page_table, kv.lens, mass, out.page_table, out.lens, out.mass, out.freed, out.n_freed, out.workspace)
+    _check("slicer_kv_evict", load().slicer_kv_evict(
+        C.byref(c), mass.data_ptr(), keep_pages, sink_pages, recent_pages, out.page_table.data_ptr(), out.lens.data_ptr(), out.mass.data_ptr(),
+        out.freed.data_ptr(), out.n_freed.data_ptr(), out.workspace.data_ptr(), _stream_handle(stream)))

@@ -24,16 +24,19 @@ using namespace slicer;
 // allocate.  Every GPU the library runs on holds its own copy until the process ends.
 static __device__ __align__(256) unsigned char scratch[SLICER_STATIC_SCRATCH_BYTES];
 
-namespace {
+static thread_local int g_last_hip_error = 0;
 
-thread_local int g_last_hip_error = 0;
-thread_local hipEvent_t g_ev_start = nullptr, g_ev_stop = nullptr;
-
-inline int hip_fail(hipError_t e)
+int slicer::note_hip_error(hipError_t e)
 {
     g_last_hip_error = (int)e;
     return SLICER_EHIP;
 }
+
+namespace {
+
+thread_local hipEvent_t g_ev_start = nullptr, g_ev_stop = nullptr;
+
+inline int hip_fail(hipError_t e) { return note_hip_error(e); }
 
 #define SLICER_HIP(call)                                   \
     do {                                                   \

@@ -1,0 +1,229 @@
+// C ABI of the attention cache in 8 bits (see include/slicer.h): argument checks, workspace carving and launches.
+#include "../../include/slicer.h"
+
+#include <hip/hip_runtime.h>
+#include <algorithm>
+#include <cmath>
+
+#include "slicer_launch.hpp"
+#include "slicer_launch_kv.hpp"
+#include "slicer_kv_evict.hpp"
+
+using namespace slicer;
+
+namespace {
+
+int round32(int d) { return (d + 31) / 32 * 32; }
+
+int check_kv(const slicer_kv* kv)
+{
+    if (!kv || kv->seqs < 1 || kv->kv_heads < 1 || kv->max_pages < 1 || kv->max_pages > 1 << 24) return SLICER_EINVAL;
+    if (kv->n_pages < 1 || kv->n_pages >= (int64_t)1 << 31) return SLICER_EINVAL;
+    if ((int64_t)kv->seqs * kv->kv_heads >= (int64_t)1 << 22) return SLICER_EINVAL;
+    if (kv->head_dim < 8 || kv->head_dim > 256 || kv->head_dim % 8) return SLICER_EINVAL;
+    return SLICER_OK;
+}
+
+int check_call(const slicer_kv* kv, int dt, int64_t tokens, const int32_t* starts, int max_new)
+{
+    int rc = check_kv(kv);
+    if (rc) return rc;
+    if (dt != SLICER_F32 && dt != SLICER_BF16) return SLICER_EUNSUPPORTED;
+    if (!kv->pages || !kv->scales || !kv->tails || !kv->page_table || !kv->lens) return SLICER_EINVAL;
+    if (tokens < 0 || tokens >= (int64_t)1 << 31 || (tokens > 0 && (!starts || max_new < 1))) return SLICER_EINVAL;
+    return SLICER_OK;
+}
+
+KvView view_of(const slicer_kv* kv)
+{
+    KvView v;
+    v.pages = (uint8_t*)kv->pages;
+    v.scales = kv->scales;
+    v.tails = (uint16_t*)kv->tails;
+    v.table = kv->page_table;
+    v.lens = kv->lens;
+    v.seqs = kv->seqs;
+    v.G = kv->kv_heads;
+    v.D = kv->head_dim;
+    v.dp = round32(kv->head_dim);
+    v.max_pages = kv->max_pages;
+    v.n_pages = kv->n_pages;
+    return v;
+}
+
+// whether every row of a strided tensor may be read 16 bytes at a time
+bool wide_rows(const void* p, int dt, int64_t token, int64_t head)
+{
+    const int64_t e = dt == SLICER_F32 ? 4 : 8;
+    return ((uintptr_t)p & 15) == 0 && token % e == 0 && head % e == 0;
+}
+
+int64_t blocks_of(int64_t tokens, int max_new) { return (std::min<int64_t>(tokens, max_new) + kPage - 2) / kPage + 1; }
+
+inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+struct AttendPlan {
+    int splits, rows_pad;
+    KvAttendLaunch launch;
+    size_t off_part_ml, off_part_o, off_page_w, off_row_ml, total;
+};
+
+AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_new, int64_t max_len)
+{
+    AttendPlan p;
+    const int64_t pairs = (int64_t)kv->seqs * kv->kv_heads, R = heads / kv->kv_heads;
+    const int64_t rows = std::min<int64_t>(std::min<int64_t>(tokens, max_new) * R, (int64_t)1 << 31);
+    const int64_t pages = std::min<int64_t>(kv->max_pages, (std::max<int64_t>(max_len, 1) + kPage - 1) / kPage);
+    p.rows_pad = (int)std::min<int64_t>(rows, kSplitRows);
+    p.launch.split_tiles = (p.rows_pad + 15) / 16;
+    // Four wavefronts of a workgroup take a page each; as many workgroups as the chip holds at once, and no fewer than four pages each.
+    const int64_t tiles = pairs * p.launch.split_tiles;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((1024 + tiles - 1) / tiles, (pages + 3) / 4));
+    p.launch.row_blocks = p.splits > 1 ? (p.rows_pad + 3) / 4 : 0;
+    p.launch.page_blocks = (int)((pages + 255) / 256);
+    p.launch.prompt_tiles = rows > kSplitRows ? (int)((rows + kTileRows - 1) / kTileRows) : 0;
+    p.launch.mass_tiles = (int)((pages + 3) / 4);
+    size_t o = 0;
+    const size_t slots = (size_t)pairs * p.rows_pad * p.splits;
+    p.off_part_ml = o; o += align256(slots * sizeof(float2));
+    p.off_part_o = o; o += align256(p.splits > 1 ? slots * round32(kv->head_dim) * sizeof(float) : 0);
+    p.off_page_w = o; o += align256((size_t)pairs * kv->max_pages * p.rows_pad * sizeof(float2));
+    p.off_row_ml = o; o += align256(p.launch.prompt_tiles ? (size_t)tokens * heads * sizeof(float2) : 0);
+    p.total = o;
+    return p;
+}
+
+int fail(hipError_t e) { return e == hipSuccess ? SLICER_OK : note_hip_error(e); }
+
+}  // namespace
+
+extern "C" {
+
+int slicer_kv_sizes(const slicer_kv* kv, size_t* pages_bytes, size_t* scales_bytes, size_t* tails_bytes)
+{
+    int rc = check_kv(kv);
+    if (rc) return rc;
+    const size_t dp = (size_t)round32(kv->head_dim), heads = (size_t)kv->kv_heads;
+    if (pages_bytes) *pages_bytes = (size_t)kv->n_pages * heads * 2 * kPage * dp;
+    if (scales_bytes) *scales_bytes = (size_t)kv->n_pages * heads * 2 * sizeof(float);
+    if (tails_bytes) *tails_bytes = (size_t)kv->seqs * heads * 2 * kPage * dp * sizeof(uint16_t);
+    return SLICER_OK;
+}
+
+int slicer_kv_append(const slicer_kv* kv, const void* k, const void* v, slicer_dtype dt, int64_t tokens, const int32_t* starts, int max_new,
+                     int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* hip_stream)
+{
+    int rc = check_call(kv, (int)dt, tokens, starts, max_new);
+    if (rc) return rc;
+    if (tokens == 0) return SLICER_OK;
+    if (!k || !v) return SLICER_EINVAL;
+    KvAppendArgs a;
+    a.kv = view_of(kv);
+    a.k = k;
+    a.v = v;
+    a.k_token = k_token;
+    a.k_head = k_head;
+    a.v_token = v_token;
+    a.v_head = v_head;
+    a.starts = starts;
+    a.tokens = tokens;
+    a.wide = wide_rows(k, (int)dt, k_token, k_head) && wide_rows(v, (int)dt, v_token, v_head);
+    const int64_t blocks = blocks_of(tokens, max_new);
+    return fail(dt == SLICER_F32 ? launch_kv_append<0>(a, blocks, (hipStream_t)hip_stream) : launch_kv_append<1>(a, blocks, (hipStream_t)hip_stream));
+}
+
+int slicer_kv_attend_sizes(const slicer_kv* kv, int heads, int64_t tokens, int max_new, int64_t max_len, size_t* workspace_bytes)
+{
+    int rc = check_kv(kv);
+    if (rc) return rc;
+    if (heads < 1 || heads % kv->kv_heads || tokens < 0 || tokens >= (int64_t)1 << 31 || (tokens > 0 && max_new < 1) || max_len < 0) return SLICER_EINVAL;
+    if (workspace_bytes) *workspace_bytes = tokens ? plan_attend(kv, heads, tokens, max_new, max_len).total : 0;
+    return SLICER_OK;
+}
+
+int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int heads, int64_t tokens, const int32_t* starts, int max_new,
+                     int64_t max_len, int64_t q_token, int64_t q_head, double scale, int causal, void* out, float* lse, float* mass, double mass_decay,
+                     void* workspace, void* hip_stream)
+{
+    int rc = check_call(kv, (int)dt, tokens, starts, max_new);
+    if (rc) return rc;
+    if (heads < 1 || heads % kv->kv_heads || !std::isfinite(scale) || !(mass_decay >= 0.0 && mass_decay <= 1.0) || max_len < 0) return SLICER_EINVAL;
+    if (tokens == 0) return SLICER_OK;
+    if (!q || !out || !workspace) return SLICER_EINVAL;
+    AttendPlan p = plan_attend(kv, heads, tokens, max_new, max_len);
+    const int64_t pairs = (int64_t)kv->seqs * kv->kv_heads;
+    if (!mass) p.launch.page_blocks = p.launch.mass_tiles = 0;
+    for (int64_t n : {(int64_t)p.launch.split_tiles * p.splits, (int64_t)p.launch.row_blocks + p.launch.page_blocks, (int64_t)p.launch.prompt_tiles, (int64_t)p.launch.mass_tiles})
+        if (pairs * n >= (int64_t)1 << 31) return SLICER_EINVAL;        // more workgroups than a launch can have
+    KvAttendArgs a;
+    a.kv = view_of(kv);
+    a.q = q;
+    a.q_token = q_token;
+    a.q_head = q_head;
+    a.starts = starts;
+    a.tokens = tokens;
+    a.R = heads / kv->kv_heads;
+    a.H = heads;
+    a.max_new = max_new;
+    a.causal = causal != 0;
+    a.scale = (float)(scale * 1.44269504088896340736);
+    a.out = out;
+    a.lse = lse;
+    a.mass = mass;
+    a.decay = (float)mass_decay;
+    a.wide_q = wide_rows(q, (int)dt, q_token, q_head);
+    a.splits = p.splits;
+    a.rows_pad = p.rows_pad;
+    uint8_t* ws = (uint8_t*)workspace;
+    a.part_ml = (float2*)(ws + p.off_part_ml);
+    a.part_o = (float*)(ws + p.off_part_o);
+    a.page_w = (float2*)(ws + p.off_page_w);
+    a.row_ml = (float2*)(ws + p.off_row_ml);
+    return fail(dt == SLICER_F32 ? launch_kv_attend<0>(a, p.launch, (hipStream_t)hip_stream) : launch_kv_attend<1>(a, p.launch, (hipStream_t)hip_stream));
+}
+
+int slicer_kv_read(const slicer_kv* kv, void* k, void* v, slicer_dtype dt, int64_t tokens, const int32_t* starts, int max_new, void* hip_stream)
+{
+    int rc = check_call(kv, (int)dt, tokens, starts, max_new);
+    if (rc) return rc;
+    if (tokens == 0) return SLICER_OK;
+    if (!k || !v) return SLICER_EINVAL;
+    KvReadArgs a;
+    a.kv = view_of(kv);
+    a.k = k;
+    a.v = v;
+    a.starts = starts;
+    a.tokens = tokens;
+    a.wide = (((uintptr_t)k | (uintptr_t)v) & 15) == 0;
+    const int64_t blocks = blocks_of(tokens, max_new);
+    return fail(dt == SLICER_F32 ? launch_kv_read<0>(a, blocks, (hipStream_t)hip_stream) : launch_kv_read<1>(a, blocks, (hipStream_t)hip_stream));
+}
+
+int slicer_kv_evict(const slicer_kv* kv, const float* mass, int keep_pages, int sink_pages, int recent_pages, int32_t* page_table_out, int32_t* lens_out,
+                    float* mass_out, int32_t* freed, int32_t* n_freed, void* workspace, void* hip_stream)
+{
+    int rc = check_kv(kv);
+    if (rc) return rc;
+    if (!kv->page_table || !kv->lens || !mass || !page_table_out || !lens_out || !mass_out || !freed || !n_freed || !workspace) return SLICER_EINVAL;
+    if (keep_pages < 0 || sink_pages < 0 || recent_pages < 0 || (int64_t)sink_pages + recent_pages > keep_pages) return SLICER_EINVAL;
+    KvEvictArgs a;
+    a.table = kv->page_table;
+    a.lens = kv->lens;
+    a.mass = mass;
+    a.seqs = kv->seqs;
+    a.G = kv->kv_heads;
+    a.max_pages = kv->max_pages;
+    a.keep = keep_pages;
+    a.sink = sink_pages;
+    a.recent = recent_pages;
+    a.out_table = page_table_out;
+    a.out_lens = lens_out;
+    a.out_mass = mass_out;
+    a.freed = freed;
+    a.n_freed = n_freed;
+    a.keys = (u64*)workspace;
+    hipLaunchKernelGGL(kv_evict_kernel, dim3((unsigned)kv->seqs), dim3(1024), 0, (hipStream_t)hip_stream, a);
+    return fail(hipGetLastError());
+}
+
+}  // extern "C"

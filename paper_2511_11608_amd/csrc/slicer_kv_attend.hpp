@@ -1,0 +1,786 @@
+// Attention over the cache in 8 bits (gfx950, wave64): o = softmax(scale q k^T) v with a running maximum and sum, in one pass over the pages.
+//
+// Codes enter the matrix products as they are, exact in bf16 (keys) and fp16 (values); a page's two scales are factors of its scores and of its
+// probabilities.  What a product rounds is therefore the queries (bf16 queries are exact, fp32 ones are split into three bf16 numbers) and the probabilities:
+// times 2^13 they are held in fp16 (11 bits, down to 2^-27 of the largest; fp32 outputs take a second fp16 number for the rest).  bf16
+// probabilities would have added as much error as the output's own rounding.  Scores, maxima, sums and outputs are fp32 throughout.
+// The tail's values are bf16 as they came and would not fit fp16: there the probabilities are split into bf16 numbers.
+#pragma once
+
+#include "slicer_kv.hpp"
+
+namespace slicer {
+
+// Sequences with at most this many query rows a cache head (new tokens times query heads a head) split the cache over workgroups; others take a
+// workgroup per 128 rows.
+constexpr int kSplitRows = 64;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kPBias = 13.0f;
+
+struct KvAttendArgs {
+    KvView kv;
+    const void* q;
+    int64_t q_token, q_head;
+    const int32_t* starts;
+    int64_t tokens;
+    int R, H, max_new, causal;
+    float scale;                  // of the scores, times log2(e)
+    void* out;                    // [tokens][H][D]
+    float* lse;                   // [tokens][H] or null
+    float* mass;                  // [seqs][G][max_pages] or null
+    float decay;
+    int wide_q;
+    // split rows: [row][splits] (maximum, sum), [row][splits][dp] sums of values; row = (sequence, head, row) with rows_pad rows a head
+    int splits, rows_pad;
+    float2* part_ml;
+    float* part_o;
+    float2* page_w;               // [sequence, head][max_pages][rows_pad] a page's sum of weights under a maximum
+    float2* row_ml;               // [tokens][H] (maximum, 1 / sum) of the rows that are not split
+};
+
+// queries -> bf16 operands: element j of part i
+template <int DT>
+struct QParts;
+template <>
+struct QParts<1> {
+    static constexpr int N = 1;
+    static constexpr int NP = 1;          // fp16 numbers a probability is held in
+    static constexpr int NB = 2;          // bf16 numbers
+    __device__ static inline void load(const KvAttendArgs& a, int64_t at, bf16x8* p) { p[0] = bf16_of(Row8<1>::bf16(a.q, at, a.wide_q)); }
+};
+template <>
+struct QParts<0> {
+    static constexpr int N = 3;
+    static constexpr int NP = 2;
+    static constexpr int NB = 3;
+    __device__ static inline void load(const KvAttendArgs& a, int64_t at, bf16x8* p)
+    {
+        float f[8];
+        Row8<0>::f32(a.q, at, a.wide_q, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const __bf16 h = (__bf16)f[j];
+            const float r = f[j] - (float)h;
+            const __bf16 m = (__bf16)r;
+            p[0][j] = h;
+            p[1][j] = m;
+            p[2][j] = (__bf16)(r - (float)m);
+        }
+    }
+};
+
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <int DT>
+__device__ inline void store4(void* out, int64_t at, f32x4 v)
+{
+    if constexpr (DT == 0) {
+        *(f32x4*)((float*)out + at) = v;
+    } else {
+        uint2 r;
+        const bf16x2 a = {(__bf16)v[0], (__bf16)v[1]}, b = {(__bf16)v[2], (__bf16)v[3]};
+        __builtin_memcpy(&r.x, &a, 4);
+        __builtin_memcpy(&r.y, &b, 4);
+        *(uint2*)((uint16_t*)out + at) = r;
+    }
+}
+
+// ---- few rows: the cache is split over workgroups -------------------------------------------------------------------------
+//
+// A workgroup has one cache head of one sequence, sixteen query rows and a share of the pages; its four wavefronts take pages in turn, each with
+// sums of its own, which meet in LDS at the end.  S^T = K Q^T and O^T = V^T P^T, so that a lane holds one row's scores and probabilities.  Codes go from memory to
+// registers to the matrix units; a page's values are on their way while its scores are made, the next page's keys while its values are used.
+// Memory bound: 2 * D bytes a token and head.
+template <int DT, int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void kv_split_kernel(KvAttendArgs a)
+{
+    constexpr int KS = DP / 32, DTL = DP / 16, NQ = QParts<DT>::N, NP = QParts<DT>::NP, NB = QParts<DT>::NB;
+    constexpr int LDO = DP + 4;
+    __shared__ __align__(16) float xo[4][16][LDO];
+    __shared__ float2 xml[4][16];
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 15, gq = lane >> 4;
+    const int row_tiles = (a.rows_pad + 15) / 16;
+    const int split = blockIdx.x % a.splits, rt = (blockIdx.x / a.splits) % row_tiles, bg = blockIdx.x / a.splits / row_tiles;
+    const int b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
+    KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
+    const int n_all = s.n;
+    s.n = s.n < a.max_new ? s.n : a.max_new;
+    const int rows = s.n * a.R;
+    if (rt * 16 >= rows || rows > kSplitRows) return;
+    const int rr = rt * 16 + c, qi = rr / a.R, qh = g * a.R + rr % a.R;
+    const bool live = rr < rows;
+    const int lim = !live ? 0 : a.causal ? s.len - n_all + qi + 1 : s.len;             // tokens that the row sees
+    const int last_row = min(rows, rt * 16 + 16) - 1;
+    const int most = a.causal ? max(0, s.len - n_all + last_row / a.R + 1) : s.len;
+    const int least = a.causal ? s.len - n_all + (rt * 16) / a.R + 1 : s.len;          // every row of the tile sees as many
+    const int full = s.len / kPage, units = (most + kPage - 1) / kPage;
+    const int per = (units + a.splits - 1) / a.splits, u0 = split * per, u1 = min(units, u0 + per);
+    const int64_t slot0 = ((int64_t)bg * a.rows_pad + rt * 16) * a.splits + split;      // of the tile's first row
+    if (u0 >= u1 && a.splits > 1) {
+        if (tid < 16 && rt * 16 + tid < rows) a.part_ml[slot0 + (int64_t)tid * a.splits] = float2{-__builtin_inff(), 0.0f};
+        return;
+    }
+
+    bf16x8 q[NQ][KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+        bf16x8 p[NQ];
+        const int d = k * 32 + gq * 8;
+        if (live && d < D) QParts<DT>::load(a, (s.first + qi) * a.q_token + qh * a.q_head + d, p);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) q[i][k] = live && d < D ? p[i] : bf16x8{};
+    }
+
+    float m = -__builtin_inff(), l = 0.0f;               // of the lane's row; l: of the lane's own tokens
+    f32x4 o[DTL];
+#pragma unroll
+    for (int t = 0; t < DTL; ++t) o[t] = f32x4{0, 0, 0, 0};
+    float2* const page_w = a.page_w + (int64_t)bg * a.kv.max_pages * a.rows_pad;
+
+    // scores of a page -> probabilities (times 2^13), the running maximum and sum; returns what the sums so far are to be multiplied by
+    auto softmax = [&](f32x4* sc, float factor, int u) {
+        const int base = u * kPage;
+        float mx = -__builtin_inff();
+        if (base + kPage <= least) {
+#pragma unroll
+            for (int T = 0; T < 4; ++T)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) { sc[T][r] *= factor; mx = fmaxf(mx, sc[T][r]); }
+        } else {
+#pragma unroll
+            for (int T = 0; T < 4; ++T)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    sc[T][r] = base + T * 16 + gq * 4 + r < lim ? sc[T][r] * factor : -__builtin_inff();
+                    mx = fmaxf(mx, sc[T][r]);
+                }
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mn = fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.0f : mn;
+        const float alpha = exp2_of(m - ms), off = kPBias - ms;
+        float sum = 0.0f;
+#pragma unroll
+        for (int T = 0; T < 4; ++T)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { sc[T][r] = exp2_of(sc[T][r] + off); sum += sc[T][r]; }
+        m = mn;
+        l = __builtin_fmaf(l, alpha, sum);
+        if (a.mass) {
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (gq == 0 && live) page_w[(int64_t)u * a.rows_pad + rr] = float2{ms, sum};
+        }
+        return alpha;
+    };
+
+    // this wavefront's pages: u0 + wid, u0 + wid + 4, ...; places and scales of the next 64 of them lie in the lanes
+    const int ufull = min(u1, full);
+    int64_t my_page = 0;
+    float my_ks = 0.0f, my_vs = 0.0f;
+    auto fetch = [&](int u) {                            // lane i: page u + 4 i
+        const int up = u + 4 * lane;
+        my_page = 0;
+        my_ks = my_vs = 0.0f;
+        if (up < ufull) {
+            const int64_t id = a.kv.table[(int64_t)b * a.kv.max_pages + up];
+            const bool there = id >= 0 && id < a.kv.n_pages;
+            my_page = there ? id : 0;
+            const float2 sc = *(const float2*)(a.kv.scales + (my_page * a.kv.G + g) * 2);
+            my_ks = there ? sc.x : __uint_as_float(0x7FC00000u);       // a page that is not there: NaN for who sees it
+            my_vs = sc.y;
+        }
+    };
+    auto record = [&](int i) {
+        const u32 id = bcast((u32)my_page, i);
+        return (const uint4*)(a.kv.pages + kv_record(a.kv, id, g)) + lane;
+    };
+    int u = u0 + wid;
+    uint4 kb[2 * KS], vb[DTL];
+    const uint4* rec = nullptr;
+    if (u < ufull) {
+        fetch(u);
+        rec = record(0);
+#pragma unroll
+        for (int i = 0; i < 2 * KS; ++i) kb[i] = rec[i * 64];
+    }
+    for (int it = 0; u < ufull; u += 4, ++it) {
+        const float ks = __uint_as_float(bcast(__float_as_uint(my_ks), it & 63)) * a.scale, vs = __uint_as_float(bcast(__float_as_uint(my_vs), it & 63));
+#pragma unroll
+        for (int i = 0; i < DTL; ++i) vb[i] = rec[(2 * KS + i) * 64];
+        f32x4 sc[4];
+#pragma unroll
+        for (int T = 0; T < 4; ++T) sc[T] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int T2 = 0; T2 < 2; ++T2)
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const uint4 w = kb[T2 * KS + k];
+                const bf16x8 k0 = codes_bf16(w.x, w.y), k1 = codes_bf16(w.z, w.w);
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) {
+                    sc[2 * T2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[i][k], sc[2 * T2], 0, 0, 0);
+                    sc[2 * T2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][k], sc[2 * T2 + 1], 0, 0, 0);
+                }
+            }
+        if (u + 4 < ufull) {
+            if ((it & 63) == 63) fetch(u + 4);
+            rec = record((it + 1) & 63);
+#pragma unroll
+            for (int i = 0; i < 2 * KS; ++i) kb[i] = rec[i * 64];
+        }
+        const float alpha = softmax(sc, ks, u);
+        f16x8 p[NP][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float f = sc[2 * h + (j >> 2)][j & 3];
+                const _Float16 hi = (_Float16)f;
+                p[0][h][j] = hi;
+                if constexpr (NP > 1) p[1][h][j] = (_Float16)(f - (float)hi);
+            }
+#pragma unroll
+        for (int t = 0; t < DTL; ++t) {
+            const f16x8 v0 = f16_of(codes_f16(vb[t].x), codes_f16(vb[t].y)), v1 = f16_of(codes_f16(vb[t].z), codes_f16(vb[t].w));
+            f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[i][0], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[i][1], acc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[t][r] = __builtin_fmaf(acc[r], vs, o[t][r] * alpha);
+        }
+    }
+    if (u < u1 && u == full) {                           // the tail, as the last page
+        const int count = s.len - full * kPage;
+        const uint16_t* tk = a.kv.tails + kv_tail(a.kv, b, g);
+        const uint16_t* tv = tk + kPage * DP;
+        f32x4 sc[4];
+#pragma unroll
+        for (int T = 0; T < 4; ++T) {
+            sc[T] = f32x4{0, 0, 0, 0};
+            if (T * 16 < count) {
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    const bf16x8 w = bf16_of(*(const uint4*)(tk + (T * 16 + c) * DP + k * 32 + gq * 8));
+#pragma unroll
+                    for (int i = 0; i < NQ; ++i) sc[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, q[i][k], sc[T], 0, 0, 0);
+                }
+            }
+        }
+        const float alpha = softmax(sc, a.scale, u);
+        bf16x8 p[NB][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float f = sc[2 * h + (j >> 2)][j & 3];
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    p[i][h][j] = (__bf16)f;
+                    f -= (float)p[i][h][j];
+                }
+            }
+#pragma unroll
+        for (int t = 0; t < DTL; ++t) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[t][r] *= alpha;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32 w[4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {            // four tokens of an element; those behind the last are whatever the memory held
+                    const int t0 = (2 * h + e) * 16 + gq * 4;
+                    uint2 r = {0, 0};
+                    if (t0 < count) r = *(const uint2*)(tv + ((t0 >> 2) * DP + t * 16 + c) * 4);
+                    const int left = count - t0;
+                    w[2 * e] = left >= 2 ? r.x : left == 1 ? r.x & 0xFFFFu : 0u;
+                    w[2 * e + 1] = left >= 4 ? r.y : left == 3 ? r.y & 0xFFFFu : 0u;
+                }
+                const bf16x8 v = bf16_of(uint4{w[0], w[1], w[2], w[3]});
+#pragma unroll
+                for (int i = 0; i < NB; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[i][h], o[t], 0, 0, 0);
+            }
+        }
+    }
+
+    // the four wavefronts' sums under one maximum
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (gq == 0) xml[wid][c] = float2{m, l};
+    __syncthreads();
+    float M = fmaxf(fmaxf(xml[0][c].x, xml[1][c].x), fmaxf(xml[2][c].x, xml[3][c].x));
+    const float Ms = M == -__builtin_inff() ? 0.0f : M;
+    const float f = exp2_of(m - Ms);
+#pragma unroll
+    for (int t = 0; t < DTL; ++t) *(f32x4*)&xo[wid][c][t * 16 + gq * 4] = o[t] * f;
+    float L = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) L += xml[w][c].y * exp2_of(xml[w][c].x - Ms);
+    __syncthreads();
+    // xml again: maximum and sum of the rows
+    if (wid == 0 && gq == 0) xml[0][c] = float2{M, L};
+    __syncthreads();
+    for (int i = tid; i < 16 * (DP / 4); i += 256) {
+        const int r = i / (DP / 4), d = i % (DP / 4) * 4;
+        if (rt * 16 + r >= rows || d >= D) continue;
+        f32x4 v = *(const f32x4*)&xo[0][r][d];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) v += *(const f32x4*)&xo[w][r][d];
+        if (a.splits > 1) {
+            *(f32x4*)(a.part_o + (slot0 + (int64_t)r * a.splits) * DP + d) = v;
+        } else {
+            const float inv = xml[0][r].y == 0.0f ? 0.0f : 1.0f / xml[0][r].y;
+            const int rw = rt * 16 + r;
+            store4<DT>(a.out, ((s.first + rw / a.R) * a.H + g * a.R + rw % a.R) * (int64_t)D + d, v * inv);
+        }
+    }
+    if (tid < 16 && rt * 16 + tid < rows) {
+        const float2 ml = xml[0][tid];
+        const int rw = rt * 16 + tid;
+        if (a.splits > 1 || a.mass) a.part_ml[slot0 + (int64_t)tid * a.splits] = ml;
+        if (a.splits == 1 && a.lse) a.lse[(s.first + rw / a.R) * a.H + g * a.R + rw % a.R] = ml.y == 0.0f ? -__builtin_inff() : (ml.x - kPBias + __log2f(ml.y)) * kLn2;
+    }
+}
+
+// What the workgroups of a split sequence left is put together: outputs by row, and the pages' weights, which can only be told now that the
+// rows' sums are known.  The first row_blocks workgroups of a head have four rows each, the others 256 pages each.
+template <int DT, int DP>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_blocks, int page_blocks)
+{
+    __shared__ float2 xml[kSplitRows];
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    const int blk = blockIdx.x % (row_blocks + page_blocks), bg = blockIdx.x / (row_blocks + page_blocks);
+    const int b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
+    KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
+    const int n_all = s.n;
+    s.n = s.n < a.max_new ? s.n : a.max_new;
+    const int rows = s.n * a.R;
+    if (rows == 0 || rows > kSplitRows) return;
+    auto total = [&](int r) {                            // (maximum, sum) of a row
+        const float2* ml = a.part_ml + ((int64_t)bg * a.rows_pad + r) * a.splits;
+        float M = -__builtin_inff(), L = 0.0f;
+        for (int i = 0; i < a.splits; ++i) M = fmaxf(M, ml[i].x);
+        if (M == -__builtin_inff()) M = 0.0f;
+        for (int i = 0; i < a.splits; ++i) L += ml[i].y * exp2_of(ml[i].x - M);
+        return float2{M, L};
+    };
+    if (blk < row_blocks) {
+        const int r = blk * 4 + wid;
+        if (r >= rows || a.splits == 1) return;
+        const float2 ml = total(r);
+        const float inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
+        const int64_t at = (s.first + r / a.R) * a.H + g * a.R + r % a.R, slot = ((int64_t)bg * a.rows_pad + r) * a.splits;
+        if (lane * 4 < D) {
+            f32x4 v = {0, 0, 0, 0};
+            for (int i = 0; i < a.splits; ++i) {
+                const float2 p = a.part_ml[slot + i];
+                if (p.y == 0.0f) continue;               // (nothing was written there)
+                v += *(const f32x4*)(a.part_o + (slot + i) * DP + lane * 4) * exp2_of(p.x - ml.x);
+            }
+            store4<DT>(a.out, at * D + lane * 4, v * inv);
+        }
+        if (lane == 0 && a.lse) a.lse[at] = ml.y == 0.0f ? -__builtin_inff() : (ml.x - kPBias + __log2f(ml.y)) * kLn2;
+        return;
+    }
+    if (tid < rows) xml[tid] = total(tid);
+    __syncthreads();
+    for (int p = (blk - row_blocks) * 256 + tid; p < (s.len + kPage - 1) / kPage; p += page_blocks * 256) {
+        const float2* w = a.page_w + ((int64_t)bg * a.kv.max_pages + p) * a.rows_pad;
+        float sum = 0.0f;
+        for (int r = 0; r < rows; ++r) {
+            // a row's tile came to the pages that the tile's last row sees some token of
+            const int top = a.causal ? s.len - n_all + min(rows - 1, r | 15) / a.R + 1 : s.len;
+            if (p * kPage >= top || w[r].y == 0.0f) continue;
+            sum += w[r].y * exp2_of(w[r].x - xml[r].x) / xml[r].y;
+        }
+        float* to = a.mass + (int64_t)bg * a.kv.max_pages + p;
+        *to = a.decay == 0.0f ? sum : __builtin_fmaf(*to, a.decay, sum);
+    }
+}
+
+// ---- many rows: a workgroup per 128 of them --------------------------------------------------------------------------------
+//
+// Four wavefronts of 32 rows (token after token, a token's query heads of the cache head next to each other) share the pages: a page's codes are loaded one
+// page ahead, turned into bf16 and fp16 operands once for all four and read from LDS as the lanes want them.  S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16
+// products, a lane has the scores of one row.  Bound by the matrix units, the exponentials and LDS reads, in about equal parts.
+constexpr int kTileRows = 128;
+
+template <int DP>
+struct PromptTile {
+    static constexpr int KK = DP / 16, DL = DP / 32;
+    // elements of a page as operands: keys [2][KK][64 lanes][8], values [DL][4][64][8]
+    static constexpr int kKeys = 2 * KK * 64 * 8, kAll = 2 * kKeys;
+};
+
+// record -> operands of 32 x 32 x 16 products in LDS (record i of 16 bytes)
+template <int DP>
+__device__ inline void stage_keys(uint16_t* to, int i, uint4 w)
+{
+    constexpr int KK = DP / 16;
+    const int l = i & 63, st = i >> 6, T2 = st / (DP / 32), sl = st % (DP / 32), gq = l >> 4, cc = l & 15;
+    uint16_t* f = to + (((T2 * KK + sl * 2 + (gq >> 1)) * 64) + (gq & 1) * 32 + cc) * 8;
+    *(bf16x8*)f = codes_bf16(w.x, w.y);
+    *(bf16x8*)(f + 16 * 8) = codes_bf16(w.z, w.w);
+}
+
+template <int DP>
+__device__ inline void stage_values(uint16_t* to, int i, uint4 w)
+{
+    const int l = i & 63, dt = i >> 6, gq = l >> 4, cc = l & 15;
+    uint16_t* f = to + (((dt >> 1) * 4) * 64 + (gq & 1) * 32 + (dt & 1) * 16 + cc) * 8 + (gq >> 1) * 4;
+#pragma unroll
+    for (int T = 0; T < 4; ++T) *(uint2*)(f + T * 64 * 8) = codes_f16((&w.x)[T]);
+}
+
+// the tail: bf16 operands, nothing behind its last token
+template <int DP>
+__device__ inline void stage_tail(uint16_t* keys, uint16_t* values, const uint16_t* tk, int count, int tid)
+{
+    constexpr int KK = DP / 16;
+    const uint16_t* tv = tk + kPage * DP;
+    for (int i = tid; i < 2 * KK * 64; i += 256) {
+        const int l = i & 63, kk = (i >> 6) % KK, tt = (i >> 6) / KK, t = tt * 32 + (l & 31);
+        uint4 w = {0, 0, 0, 0};
+        if (t < count) w = *(const uint4*)(tk + t * DP + kk * 16 + (l >> 5) * 8);
+        *(uint4*)(keys + (size_t)i * 8) = w;
+    }
+    for (int i = tid; i < (DP / 32) * 4 * 64; i += 256) {
+        const int l = i & 63, kk = (i >> 6) & 3, dl = i >> 8, d = dl * 32 + (l & 31);
+        u32 w[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {                    // tokens (kk/2) 32 + 8 (2 (kk%2) + e) + 4 (lane/32) + 0..3
+            const int t0 = (kk >> 1) * 32 + 8 * (2 * (kk & 1) + e) + 4 * (l >> 5), left = count - t0;
+            uint2 r = {0, 0};
+            if (left > 0) r = *(const uint2*)(tv + ((t0 >> 2) * DP + d) * 4);
+            w[2 * e] = left >= 2 ? r.x : left == 1 ? r.x & 0xFFFFu : 0u;
+            w[2 * e + 1] = left >= 4 ? r.y : left == 3 ? r.y & 0xFFFFu : 0u;
+        }
+        *(uint4*)(values + (size_t)i * 8) = uint4{w[0], w[1], w[2], w[3]};
+    }
+}
+
+template <int DT, int DP>
+__global__ __launch_bounds__(256, 1) void kv_prompt_kernel(KvAttendArgs a, int row_tiles)
+{
+    constexpr int KK = DP / 16, DL = DP / 32, NQ = QParts<DT>::N, NP = QParts<DT>::NP, NB = QParts<DT>::NB;
+    constexpr int NR = (4 * DP + 255) / 256;             // records of keys (and of values) a thread
+    __shared__ __align__(16) uint16_t x[2][PromptTile<DP>::kAll];
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 31, h = lane >> 5;
+    // the longest tiles first; a head's tiles on one XCD (workgroup i runs on XCD i % 8), whose L2 its pages then are in
+    const int heads = a.kv.seqs * a.kv.G, bg = blockIdx.x % heads, rt = row_tiles - 1 - (int)(blockIdx.x / heads);
+    const int b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
+    KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
+    const int n_all = s.n;
+    s.n = s.n < a.max_new ? s.n : a.max_new;
+    const int64_t rows = (int64_t)s.n * a.R;
+    if (rows <= kSplitRows || (int64_t)rt * kTileRows >= rows) return;
+    const int64_t rr = (int64_t)rt * kTileRows + wid * 32 + c;
+    const bool live = rr < rows;
+    const int qi = (int)((live ? rr : rows - 1) / a.R), qh = g * a.R + (int)((live ? rr : rows - 1) % a.R);
+    const int lim = !live ? 0 : a.causal ? s.len - n_all + qi + 1 : s.len;
+    const int64_t last_row = min(rows, (int64_t)(rt + 1) * kTileRows) - 1;
+    const int most = a.causal ? max(0, s.len - n_all + (int)(last_row / a.R) + 1) : s.len;
+    const int least = a.causal ? s.len - n_all + (int)((int64_t)rt * kTileRows / a.R) + 1 : s.len;
+    const int full = s.len / kPage, units = (most + kPage - 1) / kPage, ufull = min(units, full);
+    const int32_t* table = a.kv.table + (int64_t)b * a.kv.max_pages;
+
+    bf16x8 q[NQ][KK];
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+        bf16x8 p[NQ];
+        const int d = k * 16 + h * 8;
+        if (live && d < D) QParts<DT>::load(a, (s.first + qi) * a.q_token + qh * a.q_head + d, p);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) q[i][k] = live && d < D ? p[i] : bf16x8{};
+    }
+
+    // outputs are held in units of vref, the scale of some page; the same in all wavefronts
+    float m = -__builtin_inff(), l = 0.0f, vref = 0.0f, vmax = 0.0f;
+    f32x16 o[DL];
+#pragma unroll
+    for (int t = 0; t < DL; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+
+    auto scores = [&](const uint16_t* keys, f32x16* sc) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[t][r] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KK; ++k)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const bf16x8 w = *(const bf16x8*)(keys + ((t * KK + k) * 64 + lane) * 8);
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[i][k], sc[t], 0, 0, 0);
+            }
+    };
+    auto softmax = [&](f32x16* sc, float factor, int u) {
+        const int base = u * kPage + h * 4;
+        float mx = -__builtin_inff();
+        if (u * kPage + kPage <= least) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) { sc[t][r] *= factor; mx = fmaxf(mx, sc[t][r]); }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    sc[t][r] = base + t * 32 + (r >> 2) * 8 + (r & 3) < lim ? sc[t][r] * factor : -__builtin_inff();
+                    mx = fmaxf(mx, sc[t][r]);
+                }
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mn = fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.0f : mn;
+        const float alpha = exp2_of(m - ms), off = kPBias - ms;
+        float sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) { sc[t][r] = exp2_of(sc[t][r] + off); sum += sc[t][r]; }
+        if (__any(mn > m)) {
+#pragma unroll
+            for (int t = 0; t < DL; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[t][r] *= alpha;
+        }
+        m = mn;
+        l = __builtin_fmaf(l, alpha, sum);
+    };
+    auto rescale = [&](float f) {
+#pragma unroll
+        for (int t = 0; t < DL; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[t][r] *= f;
+    };
+
+    uint4 kb[NR], vb[NR];
+    float ks = 0.0f, vs = 0.0f, ks_next = 0.0f, vs_next = 0.0f;
+    auto load = [&](int u) {
+        int64_t id = table[u];
+        const bool there = id >= 0 && id < a.kv.n_pages;
+        if (!there) id = 0;
+        const uint4* rec = (const uint4*)(a.kv.pages + kv_record(a.kv, id, g));
+        const float2 sc = *(const float2*)(a.kv.scales + (id * a.kv.G + g) * 2);
+        ks_next = there ? sc.x : __uint_as_float(0x7FC00000u);
+        vs_next = sc.y;
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+            if (i * 256 + tid < 4 * DP) {
+                kb[i] = rec[i * 256 + tid];
+                vb[i] = rec[4 * DP + i * 256 + tid];
+            }
+    };
+    auto stage = [&](uint16_t* to) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+            if (i * 256 + tid < 4 * DP) {
+                stage_keys<DP>(to, i * 256 + tid, kb[i]);
+                stage_values<DP>(to + PromptTile<DP>::kKeys, i * 256 + tid, vb[i]);
+            }
+    };
+    if (ufull > 0) {
+        load(0);
+        stage(x[0]);
+    }
+    for (int u = 0; u < ufull; ++u) {
+        ks = ks_next;
+        vs = vs_next;
+        __syncthreads();
+        if (u + 1 < ufull) load(u + 1);
+        const uint16_t *keys = x[u & 1], *values = keys + PromptTile<DP>::kKeys;
+        f32x16 sc[2];
+        scores(keys, sc);
+        softmax(sc, ks * a.scale, u);
+        // probabilities times vs / vref stay below 2^14 and keep their bits; a page of less than 2^-60 of the largest scale counts little enough
+        vmax = fmaxf(vmax, vs);
+        const float vt = fmaxf(vs, vmax * 0x1p-60f);
+        if (vs > 0.0f && (vt > 2.0f * vref || vt < vref * 0.015625f)) {
+            if (vref > 0.0f) rescale(vref / vt);
+            vref = vt;
+        }
+        const float ratio = vs > 0.0f ? vs / vref : 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            f16x8 p[NP];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float f = sc[k >> 1][(k & 1) * 8 + j] * ratio;
+                // the product is rounded to fp32 here: left alone, product and conversion become one instruction, whose result is in rare cases the other
+                // neighbour of the one that the rest is taken from, and a probability loses its second number
+                if constexpr (NP > 1) asm("" : "+v"(f));
+                const _Float16 hi = (_Float16)f;
+                p[0][j] = hi;
+                if constexpr (NP > 1) p[1][j] = (_Float16)(f - (float)hi);
+            }
+#pragma unroll
+            for (int t = 0; t < DL; ++t) {
+                const f16x8 v = *(const f16x8*)(values + ((t * 4 + k) * 64 + lane) * 8);
+#pragma unroll
+                for (int i = 0; i < NP; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[i], o[t], 0, 0, 0);
+            }
+        }
+        if (u + 1 < ufull) stage(x[(u + 1) & 1]);
+    }
+    if (units > full) {                                  // the tail
+        const int count = s.len - full * kPage;
+        __syncthreads();
+        stage_tail<DP>(x[0], x[0] + PromptTile<DP>::kKeys, a.kv.tails + kv_tail(a.kv, b, g), count, tid);
+        __syncthreads();
+        f32x16 sc[2];
+        scores(x[0], sc);
+        softmax(sc, a.scale, full);
+        rescale(vref);
+        const uint16_t* values = x[0] + PromptTile<DP>::kKeys;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            bf16x8 p[NB];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float f = sc[k >> 1][(k & 1) * 8 + j];
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    p[i][j] = (__bf16)f;
+                    f -= (float)p[i][j];
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < DL; ++t) {
+                const bf16x8 v = *(const bf16x8*)(values + ((t * 4 + k) * 64 + lane) * 8);
+#pragma unroll
+                for (int i = 0; i < NB; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i], o[t], 0, 0, 0);
+            }
+        }
+    }
+    l += __shfl_xor(l, 32);
+    if (!live) return;
+    const float inv = l == 0.0f ? 0.0f : (units > full ? 1.0f : vref) / l;
+    const int64_t at = (s.first + qi) * a.H + qh;
+#pragma unroll
+    for (int t = 0; t < DL; ++t)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int d = t * 32 + k * 8 + h * 4;
+            if (d < D) store4<DT>(a.out, at * D + d, f32x4{o[t][k * 4], o[t][k * 4 + 1], o[t][k * 4 + 2], o[t][k * 4 + 3]} * inv);
+        }
+    if (h == 0) {
+        const float ms = m == -__builtin_inff() ? 0.0f : m;
+        if (a.lse) a.lse[at] = l == 0.0f ? -__builtin_inff() : (ms - kPBias + __log2f(l)) * kLn2;
+        if (a.mass) a.row_ml[at] = float2{ms, l == 0.0f ? 0.0f : 1.0f / l};
+    }
+}
+
+// Weights of the pages for the rows that are not split: a column's sum needs the rows' final sums, so scores are made once more (no second product, no
+// maximum).  A wavefront has a page, its keys in registers; four of them share the query rows, 32 at a time through LDS.  Every page has one
+// wavefront: nothing is added by atomics.
+template <int DT, int DP>
+__global__ __launch_bounds__(256, 1) void kv_mass_kernel(KvAttendArgs a, int page_tiles)
+{
+    constexpr int KK = DP / 16, NQ = QParts<DT>::N;
+    __shared__ __align__(16) uint16_t xq[NQ][KK * 64 * 8];
+    __shared__ float2 xml[32];
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 31, h = lane >> 5;
+    const int bg = blockIdx.x / page_tiles, b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
+    KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
+    const int n_all = s.n;
+    s.n = s.n < a.max_new ? s.n : a.max_new;
+    const int64_t rows = (int64_t)s.n * a.R;
+    const int pages = (s.len + kPage - 1) / kPage, full = s.len / kPage;
+    if (rows <= kSplitRows) return;
+    for (int p0 = blockIdx.x % page_tiles * 4; p0 < pages; p0 += page_tiles * 4) {
+        const int p = p0 + wid;
+        bf16x8 kf[2][KK];
+        float factor = a.scale;
+        if (p < full) {
+            int64_t id = a.kv.table[(int64_t)b * a.kv.max_pages + p];
+            const bool there = id >= 0 && id < a.kv.n_pages;
+            if (!there) id = 0;
+            const uint8_t* rec = a.kv.pages + kv_record(a.kv, id, g);
+            factor *= there ? a.kv.scales[(id * a.kv.G + g) * 2] : __uint_as_float(0x7FC00000u);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int k = 0; k < KK; ++k) {
+                    // elements 16 k + 8 h + j of token 32 t + c: half c / 16 of the record of lane (2 (k % 2) + h) * 16 + c % 16
+                    const uint2 w = *(const uint2*)(rec + ((size_t)(t * (DP / 32) + (k >> 1)) * 64 + ((k & 1) * 2 + h) * 16 + (c & 15)) * 16 + (c >> 4) * 8);
+                    kf[t][k] = codes_bf16(w.x, w.y);
+                }
+        } else {
+            const uint16_t* tk = a.kv.tails + kv_tail(a.kv, b, g);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int k = 0; k < KK; ++k) {
+                    uint4 w = {0, 0, 0, 0};
+                    if (p < pages && full * kPage + t * 32 + c < s.len) w = *(const uint4*)(tk + (t * 32 + c) * DP + k * 16 + h * 8);
+                    kf[t][k] = bf16_of(w);
+                }
+        }
+        // rows before the first that sees the first page of the workgroup add nothing
+        int64_t r0 = 0;
+        if (a.causal) {
+            const int64_t i0 = (int64_t)p0 * kPage - (s.len - n_all);       // query that sees it first
+            r0 = (i0 > 0 ? i0 * a.R : 0) & ~(int64_t)31;
+        }
+        float sum = 0.0f;
+        for (; r0 < rows; r0 += 32) {
+            __syncthreads();
+            for (int i = tid; i < KK * 64; i += 256) {
+                const int ll = i & 63, k = i >> 6, d = k * 16 + (ll >> 5) * 8;
+                const int64_t r = r0 + (ll & 31);
+                bf16x8 w[NQ];
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) w[j] = bf16x8{};
+                if (r < rows && d < D) QParts<DT>::load(a, (s.first + r / a.R) * a.q_token + (g * a.R + r % a.R) * a.q_head + d, w);
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) *(bf16x8*)&xq[j][i * 8] = w[j];
+            }
+            if (tid < 32) {
+                const int64_t r = r0 + tid;
+                xml[tid] = r < rows ? a.row_ml[(s.first + r / a.R) * a.H + g * a.R + r % a.R] : float2{0.0f, 0.0f};
+            }
+            __syncthreads();
+            const int64_t r = r0 + c;
+            const int lim = r >= rows ? 0 : a.causal ? s.len - n_all + (int)(r / a.R) + 1 : s.len;
+            const float2 ml = xml[c];
+            const float off = kPBias - ml.x;
+            f32x16 sc[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sc[t][j] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KK; ++k)
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) {
+                    const bf16x8 w = *(const bf16x8*)&xq[i][(k * 64 + lane) * 8];
+                    sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0][k], w, sc[0], 0, 0, 0);
+                    sc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[1][k], w, sc[1], 0, 0, 0);
+                }
+            float part = 0.0f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float e = exp2_of(sc[t][j] * factor + off);
+                    part += p * kPage + t * 32 + (j >> 2) * 8 + h * 4 + (j & 3) < lim ? e : 0.0f;
+                }
+            // (a row that sees nothing of the page adds nothing, whatever its own sum is)
+            sum += part == 0.0f ? 0.0f : part * ml.y;
+        }
+#pragma unroll
+        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+        if (lane == 0 && p < pages) {
+            float* to = a.mass + (int64_t)bg * a.kv.max_pages + p;
+            *to = a.decay == 0.0f ? sum : __builtin_fmaf(*to, a.decay, sum);
+        }
+    }
+}
+
+}  // namespace slicer

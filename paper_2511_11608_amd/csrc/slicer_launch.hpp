@@ -15,4 +15,7 @@ struct WgLaunch { int nw, chunks, lds_bytes; };
 template <int DT, bool ASYM, int NQ> hipError_t launch_small(const SmallArgs& sa, const SmallLaunch& p, hipStream_t st);
 template <int DT, bool ASYM> hipError_t launch_wg(const SmallArgs& sa, const WgLaunch& p, hipStream_t st);
 
+// Records a failed HIP call for slicer_last_hip_error (of the calling thread) and returns SLICER_EHIP.
+int note_hip_error(hipError_t e);
+
 }  // namespace slicer

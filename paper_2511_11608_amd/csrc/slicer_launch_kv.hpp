@@ -1,0 +1,86 @@
+// Launchers of the cache's kernels, instantiated by element type (a translation unit each) and by head size rounded up to 32.
+#pragma once
+
+#include <algorithm>
+
+#include "slicer_kv_attend.hpp"
+#include "slicer_kv_cache.hpp"
+
+namespace slicer {
+
+// Workgroups of an append or a read: blocks of a sequence, and the (sequence, head) pairs over the other two dimensions.
+inline dim3 kv_grid(int64_t blocks, int64_t pairs)
+{
+    const int64_t y = std::min<int64_t>(pairs, 32768);
+    return dim3((unsigned)blocks, (unsigned)y, (unsigned)((pairs + y - 1) / y));
+}
+
+struct KvAttendLaunch {
+    int split_tiles;          // row tiles of sixteen for the sequences that are split; 0: none can be
+    int row_blocks, page_blocks;
+    int prompt_tiles;         // row tiles of 128; 0: no sequence can have that many rows
+    int mass_tiles;           // four pages each
+};
+
+template <int DT> hipError_t launch_kv_append(const KvAppendArgs& a, int64_t blocks, hipStream_t st);
+template <int DT> hipError_t launch_kv_read(const KvReadArgs& a, int64_t blocks, hipStream_t st);
+template <int DT> hipError_t launch_kv_attend(const KvAttendArgs& a, const KvAttendLaunch& p, hipStream_t st);
+
+#ifdef SLICER_KV_INSTANTIATE
+
+template <typename F>
+inline void kv_by_size(int dp, F f)
+{
+    switch (dp) {
+        case 32: f(std::integral_constant<int, 32>()); break;
+        case 64: f(std::integral_constant<int, 64>()); break;
+        case 96: f(std::integral_constant<int, 96>()); break;
+        case 128: f(std::integral_constant<int, 128>()); break;
+        case 160: f(std::integral_constant<int, 160>()); break;
+        case 192: f(std::integral_constant<int, 192>()); break;
+        case 224: f(std::integral_constant<int, 224>()); break;
+        default: f(std::integral_constant<int, 256>()); break;
+    }
+}
+
+template <int DT>
+hipError_t launch_kv_append(const KvAppendArgs& a, int64_t blocks, hipStream_t st)
+{
+    kv_by_size(a.kv.dp, [&](auto dp) {
+        hipLaunchKernelGGL((kv_append_kernel<DT, decltype(dp)::value>), kv_grid(blocks, (int64_t)a.kv.seqs * a.kv.G), dim3(256), 0, st, a);
+    });
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_kv_read(const KvReadArgs& a, int64_t blocks, hipStream_t st)
+{
+    kv_by_size(a.kv.dp, [&](auto dp) {
+        hipLaunchKernelGGL((kv_read_kernel<DT, decltype(dp)::value>), kv_grid(blocks, (int64_t)a.kv.seqs * a.kv.G), dim3(256), 0, st, a);
+    });
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_kv_attend(const KvAttendArgs& a, const KvAttendLaunch& p, hipStream_t st)
+{
+    const unsigned pairs = (unsigned)(a.kv.seqs * a.kv.G);
+    kv_by_size(a.kv.dp, [&](auto dp) {
+        constexpr int DP = decltype(dp)::value;
+        if (p.split_tiles) {
+            hipLaunchKernelGGL((kv_split_kernel<DT, DP>), dim3(pairs * (unsigned)(p.split_tiles * a.splits)), dim3(256), 0, st, a);
+            if (p.row_blocks + p.page_blocks)
+                hipLaunchKernelGGL((kv_join_kernel<DT, DP>), dim3(pairs * (unsigned)(p.row_blocks + p.page_blocks)), dim3(256), 0, st, a, p.row_blocks, p.page_blocks);
+        }
+        if (p.prompt_tiles) {
+            hipLaunchKernelGGL((kv_prompt_kernel<DT, DP>), dim3(pairs * (unsigned)p.prompt_tiles), dim3(256), 0, st, a, p.prompt_tiles);
+            if (p.mass_tiles)
+                hipLaunchKernelGGL((kv_mass_kernel<DT, DP>), dim3(pairs * (unsigned)p.mass_tiles), dim3(256), 0, st, a, p.mass_tiles);
+        }
+    });
+    return hipGetLastError();
+}
+
+#endif
+
+}  // namespace slicer
