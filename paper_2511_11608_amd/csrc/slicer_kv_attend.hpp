@@ -14,7 +14,9 @@ namespace slicer {
 // Sequences with at most this many query rows a cache head (new tokens times query heads a head) split the cache over workgroups; others take a
 // workgroup per 128 rows.
 constexpr int kSplitRows = 64;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+// Tables of at most this many pages: weights of rows that one workgroup has all of are made where they arise.
+constexpr int kMassPages = 64;
+constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kPBias = 13.0f;
 
 struct KvAttendArgs {
@@ -92,16 +94,23 @@ __device__ inline void store4(void* out, int64_t at, f32x4 v)
 // registers to the matrix units; a page's values are on their way while its scores are made, the next page's keys while its values are used.
 // Memory bound: 2 * D bytes a token and head.
 template <int DT, int DP>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void kv_split_kernel(KvAttendArgs a)
+__global__ __launch_bounds__(256, DP <= 160 || (DP == 192 && DT == 1) ? 2 : 1) void kv_split_kernel(KvAttendArgs a)
 {
     constexpr int KS = DP / 32, DTL = DP / 16, NQ = QParts<DT>::N, NP = QParts<DT>::NP, NB = QParts<DT>::NB;
     constexpr int LDO = DP + 4;
     __shared__ __align__(16) float xo[4][16][LDO];
     __shared__ float2 xml[4][16];
+    __shared__ float2 xw[kMassPages * 16];               // a page's sums of weights under a maximum, where all of them are here
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 15, gq = lane >> 4;
     const int row_tiles = (a.rows_pad + 15) / 16;
     const int split = blockIdx.x % a.splits, rt = (blockIdx.x / a.splits) % row_tiles, bg = blockIdx.x / a.splits / row_tiles;
     const int b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
+    const bool own_mass = a.mass && a.splits == 1 && row_tiles == 1 && a.kv.max_pages <= kMassPages;
+    // places of this wavefront's pages: those of the next 64 lie in the lanes.  Where the first is known before the length, they are asked for at once
+    // (a workgroup starts with a chain of dependent loads, 1 us each under load: length, place, codes)
+    const int32_t* const table = a.kv.table + (int64_t)b * a.kv.max_pages;
+    int early = -1;
+    if (a.splits == 1 && wid + 4 * lane < a.kv.max_pages) early = table[wid + 4 * lane];
     KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
     const int n_all = s.n;
     s.n = s.n < a.max_new ? s.n : a.max_new;
@@ -169,21 +178,24 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void kv_split_kernel(KvAtte
         if (a.mass) {
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
-            if (gq == 0 && live) page_w[(int64_t)u * a.rows_pad + rr] = float2{ms, sum};
+            if (gq == 0 && live) {
+                if (own_mass) xw[u * 16 + c] = float2{ms, sum};
+                else page_w[(int64_t)u * a.rows_pad + rr] = float2{ms, sum};
+            }
         }
         return alpha;
     };
 
-    // this wavefront's pages: u0 + wid, u0 + wid + 4, ...; places and scales of the next 64 of them lie in the lanes
+    // this wavefront's pages: u0 + wid, u0 + wid + 4, ...
     const int ufull = min(u1, full);
     int64_t my_page = 0;
     float my_ks = 0.0f, my_vs = 0.0f;
-    auto fetch = [&](int u) {                            // lane i: page u + 4 i
+    auto fetch = [&](int u, bool known) {                // lane i: page u + 4 i
         const int up = u + 4 * lane;
         my_page = 0;
         my_ks = my_vs = 0.0f;
         if (up < ufull) {
-            const int64_t id = a.kv.table[(int64_t)b * a.kv.max_pages + up];
+            const int64_t id = known ? early : table[up];
             const bool there = id >= 0 && id < a.kv.n_pages;
             my_page = there ? id : 0;
             const float2 sc = *(const float2*)(a.kv.scales + (my_page * a.kv.G + g) * 2);
@@ -199,7 +211,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void kv_split_kernel(KvAtte
     uint4 kb[2 * KS], vb[DTL];
     const uint4* rec = nullptr;
     if (u < ufull) {
-        fetch(u);
+        fetch(u, a.splits == 1);
         rec = record(0);
 #pragma unroll
         for (int i = 0; i < 2 * KS; ++i) kb[i] = rec[i * 64];
@@ -224,7 +236,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void kv_split_kernel(KvAtte
                 }
             }
         if (u + 4 < ufull) {
-            if ((it & 63) == 63) fetch(u + 4);
+            if ((it & 63) == 63) fetch(u + 4, false);
             rec = record((it + 1) & 63);
 #pragma unroll
             for (int i = 0; i < 2 * KS; ++i) kb[i] = rec[i * 64];
@@ -311,17 +323,18 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void kv_split_kernel(KvAtte
     l += __shfl_xor(l, 32);
     if (gq == 0) xml[wid][c] = float2{m, l};
     __syncthreads();
-    float M = fmaxf(fmaxf(xml[0][c].x, xml[1][c].x), fmaxf(xml[2][c].x, xml[3][c].x));
-    const float Ms = M == -__builtin_inff() ? 0.0f : M;
-    const float f = exp2_of(m - Ms);
+    auto total = [&](int r) {                            // (maximum, sum) of a row of the tile
+        const float M = fmaxf(fmaxf(xml[0][r].x, xml[1][r].x), fmaxf(xml[2][r].x, xml[3][r].x)), Ms = M == -__builtin_inff() ? 0.0f : M;
+        float L = 0.0f;
 #pragma unroll
-    for (int t = 0; t < DTL; ++t) *(f32x4*)&xo[wid][c][t * 16 + gq * 4] = o[t] * f;
-    float L = 0.0f;
+        for (int w = 0; w < 4; ++w) L += xml[w][r].y * exp2_of(xml[w][r].x - Ms);
+        return float2{M, L};
+    };
+    {
+        const float M = total(c).x, f = exp2_of(m - (M == -__builtin_inff() ? 0.0f : M));
 #pragma unroll
-    for (int w = 0; w < 4; ++w) L += xml[w][c].y * exp2_of(xml[w][c].x - Ms);
-    __syncthreads();
-    // xml again: maximum and sum of the rows
-    if (wid == 0 && gq == 0) xml[0][c] = float2{M, L};
+        for (int t = 0; t < DTL; ++t) *(f32x4*)&xo[wid][c][t * 16 + gq * 4] = o[t] * f;
+    }
     __syncthreads();
     for (int i = tid; i < 16 * (DP / 4); i += 256) {
         const int r = i / (DP / 4), d = i % (DP / 4) * 4;
@@ -332,25 +345,59 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void kv_split_kernel(KvAtte
         if (a.splits > 1) {
             *(f32x4*)(a.part_o + (slot0 + (int64_t)r * a.splits) * DP + d) = v;
         } else {
-            const float inv = xml[0][r].y == 0.0f ? 0.0f : 1.0f / xml[0][r].y;
+            const float L = total(r).y;
             const int rw = rt * 16 + r;
-            store4<DT>(a.out, ((s.first + rw / a.R) * a.H + g * a.R + rw % a.R) * (int64_t)D + d, v * inv);
+            store4<DT>(a.out, ((s.first + rw / a.R) * a.H + g * a.R + rw % a.R) * (int64_t)D + d, v * (L == 0.0f ? 0.0f : 1.0f / L));
         }
     }
     if (tid < 16 && rt * 16 + tid < rows) {
-        const float2 ml = xml[0][tid];
+        const float2 ml = total(tid);
         const int rw = rt * 16 + tid;
-        if (a.splits > 1 || a.mass) a.part_ml[slot0 + (int64_t)tid * a.splits] = ml;
+        if (a.splits > 1 || (a.mass && !own_mass)) a.part_ml[slot0 + (int64_t)tid * a.splits] = ml;
         if (a.splits == 1 && a.lse) a.lse[(s.first + rw / a.R) * a.H + g * a.R + rw % a.R] = ml.y == 0.0f ? -__builtin_inff() : (ml.x - kPBias + __log2f(ml.y)) * kLn2;
+    }
+    if (own_mass) {                                      // sixteen lanes a page
+        const float2 ml = total(c);
+        const int pages = (s.len + kPage - 1) / kPage;
+        for (int p = tid >> 4; p < pages; p += 16) {
+            float sum = 0.0f;
+            if (p < units && live) {
+                const float2 w = xw[p * 16 + c];
+                if (w.y != 0.0f) sum = w.y * exp2_of(w.x - ml.x) / ml.y;
+            }
+#pragma unroll
+            for (int o = 8; o; o >>= 1) sum += __shfl_xor(sum, o);
+            if (c == 0) {
+                float* to = a.mass + (int64_t)bg * a.kv.max_pages + p;
+                *to = a.decay == 0.0f ? sum : __builtin_fmaf(*to, a.decay, sum);
+            }
+        }
     }
 }
 
-// What the workgroups of a split sequence left is put together: outputs by row, and the pages' weights, which can only be told now that the
-// rows' sums are known.  The first row_blocks workgroups of a head have four rows each, the others 256 pages each.
+// (maximum, sum) of a split row from its parts, by one wavefront; every lane gets them.
+__device__ inline float2 kv_row_total(const float2* ml, int splits, int lane)
+{
+    float M = -__builtin_inff(), L = 0.0f;
+    for (int i = lane; i < splits; i += kWave) M = fmaxf(M, ml[i].x);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    if (M == -__builtin_inff()) M = 0.0f;
+    for (int i = lane; i < splits; i += kWave) L += ml[i].y * exp2_of(ml[i].x - M);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) L += __shfl_xor(L, o);
+    return float2{M, L};
+}
+
+// What the workgroups of a split sequence left is put together: outputs, a workgroup per row, and the pages' weights, which can only be told now that
+// the rows' sums are known, a workgroup per 256 pages.  A row's parts are read by all four wavefronts at once, several parts a load: with one wavefront a row, part
+// after part, 64 parts took 64 us instead of 5.
 template <int DT, int DP>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_blocks, int page_blocks)
 {
+    constexpr int LPP = DP / 4, PPW = kWave / LPP;       // lanes a part, parts a load (a part of more than 32 elements of four: one)
     __shared__ float2 xml[kSplitRows];
+    __shared__ __align__(16) float xo[4][DP];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     const int blk = blockIdx.x % (row_blocks + page_blocks), bg = blockIdx.x / (row_blocks + page_blocks);
     const int b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
@@ -359,33 +406,48 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_bl
     s.n = s.n < a.max_new ? s.n : a.max_new;
     const int rows = s.n * a.R;
     if (rows == 0 || rows > kSplitRows) return;
-    auto total = [&](int r) {                            // (maximum, sum) of a row
-        const float2* ml = a.part_ml + ((int64_t)bg * a.rows_pad + r) * a.splits;
-        float M = -__builtin_inff(), L = 0.0f;
-        for (int i = 0; i < a.splits; ++i) M = fmaxf(M, ml[i].x);
-        if (M == -__builtin_inff()) M = 0.0f;
-        for (int i = 0; i < a.splits; ++i) L += ml[i].y * exp2_of(ml[i].x - M);
-        return float2{M, L};
-    };
     if (blk < row_blocks) {
-        const int r = blk * 4 + wid;
-        if (r >= rows || a.splits == 1) return;
-        const float2 ml = total(r);
-        const float inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
-        const int64_t at = (s.first + r / a.R) * a.H + g * a.R + r % a.R, slot = ((int64_t)bg * a.rows_pad + r) * a.splits;
-        if (lane * 4 < D) {
-            f32x4 v = {0, 0, 0, 0};
-            for (int i = 0; i < a.splits; ++i) {
+        const int r = blk;
+        if (r >= rows) return;
+        const int64_t slot = ((int64_t)bg * a.rows_pad + r) * a.splits;
+        const float2 ml = kv_row_total(a.part_ml + slot, a.splits, lane);
+        const int part = PPW > 1 ? lane / LPP : 0, d = (PPW > 1 ? lane % LPP : lane) * 4;
+        f32x4 v = {0, 0, 0, 0};
+        if (part < PPW && d < D) {
+#pragma unroll 4
+            for (int i = wid * PPW + part; i < a.splits; i += 4 * PPW) {
                 const float2 p = a.part_ml[slot + i];
-                if (p.y == 0.0f) continue;               // (nothing was written there)
-                v += *(const f32x4*)(a.part_o + (slot + i) * DP + lane * 4) * exp2_of(p.x - ml.x);
+                const f32x4 x = *(const f32x4*)(a.part_o + (slot + i) * DP + d) * exp2_of(p.x - ml.x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += p.y != 0.0f ? x[e] : 0.0f;       // (a part without a sum was not written)
             }
-            store4<DT>(a.out, at * D + lane * 4, v * inv);
         }
-        if (lane == 0 && a.lse) a.lse[at] = ml.y == 0.0f ? -__builtin_inff() : (ml.x - kPBias + __log2f(ml.y)) * kLn2;
+        if constexpr (PPW > 1) {
+#pragma unroll
+            for (int q = 1; q < PPW; ++q)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float f = __shfl(v[e], (lane + q * LPP) & 63);
+                    if (part == 0) v[e] += f;
+                }
+        }
+        if (part == 0 && d < DP) *(f32x4*)&xo[wid][d] = v;
+        __syncthreads();
+        const int64_t at = (s.first + r / a.R) * a.H + g * a.R + r % a.R;
+        const float inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
+        if (tid * 4 < D) {
+            v = *(const f32x4*)&xo[0][tid * 4];
+#pragma unroll
+            for (int w = 1; w < 4; ++w) v += *(const f32x4*)&xo[w][tid * 4];
+            store4<DT>(a.out, at * D + tid * 4, v * inv);
+        }
+        if (tid == 0 && a.lse) a.lse[at] = ml.y == 0.0f ? -__builtin_inff() : (ml.x - kPBias + __log2f(ml.y)) * kLn2;
         return;
     }
-    if (tid < rows) xml[tid] = total(tid);
+    for (int r = wid; r < rows; r += 4) {
+        const float2 ml = kv_row_total(a.part_ml + ((int64_t)bg * a.rows_pad + r) * a.splits, a.splits, lane);
+        if (lane == 0) xml[r] = float2{ml.x, 1.0f / ml.y};
+    }
     __syncthreads();
     for (int p = (blk - row_blocks) * 256 + tid; p < (s.len + kPage - 1) / kPage; p += page_blocks * 256) {
         const float2* w = a.page_w + ((int64_t)bg * a.kv.max_pages + p) * a.rows_pad;
@@ -394,7 +456,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_bl
             // a row's tile came to the pages that the tile's last row sees some token of
             const int top = a.causal ? s.len - n_all + min(rows - 1, r | 15) / a.R + 1 : s.len;
             if (p * kPage >= top || w[r].y == 0.0f) continue;
-            sum += w[r].y * exp2_of(w[r].x - xml[r].x) / xml[r].y;
+            sum += w[r].y * exp2_of(w[r].x - xml[r].x) * xml[r].y;
         }
         float* to = a.mass + (int64_t)bg * a.kv.max_pages + p;
         *to = a.decay == 0.0f ? sum : __builtin_fmaf(*to, a.decay, sum);
