@@ -75,12 +75,13 @@ AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_n
     const int64_t rows = std::min<int64_t>(std::min<int64_t>(tokens, max_new) * R, (int64_t)1 << 31);
     const int64_t pages = std::min<int64_t>(kv->max_pages, (std::max<int64_t>(max_len, 1) + kPage - 1) / kPage);
     p.rows_pad = (int)std::min<int64_t>(rows, kSplitRows);
-    p.launch.split_tiles = (p.rows_pad + 15) / 16;
+    p.launch.tile_rows = p.rows_pad > 16 && round32(kv->head_dim) <= kWideTile ? 32 : 16;
+    p.launch.split_tiles = (p.rows_pad + p.launch.tile_rows - 1) / p.launch.tile_rows;
     // Four wavefronts of a workgroup take a page each; as many workgroups as the chip holds at once (two a CU), and no fewer than four pages each.
     const int64_t tiles = pairs * p.launch.split_tiles;
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((512 + tiles - 1) / tiles, (pages + 3) / 4));
     p.launch.row_blocks = p.splits > 1 ? p.rows_pad : 0;
-    p.launch.page_blocks = p.splits > 1 || p.launch.split_tiles > 1 || kv->max_pages > kMassPages ? (int)((pages + 255) / 256) : 0;
+    p.launch.page_blocks = p.splits > 1 || p.rows_pad > 16 || kv->max_pages > kMassPages ? (int)((pages + 255) / 256) : 0;
     p.launch.prompt_tiles = rows > kSplitRows ? (int)((rows + kTileRows - 1) / kTileRows) : 0;
     p.launch.mass_tiles = (int)((pages + 3) / 4);
     size_t o = 0;

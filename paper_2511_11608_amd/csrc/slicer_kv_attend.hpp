@@ -89,23 +89,24 @@ __device__ inline void store4(void* out, int64_t at, f32x4 v)
 
 // ---- few rows: the cache is split over workgroups -------------------------------------------------------------------------
 //
-// A workgroup has one cache head of one sequence, sixteen query rows and a share of the pages; its four wavefronts take pages in turn, each with
+// A workgroup has one cache head of one sequence, 16 QT query rows and a share of the pages; its four wavefronts take pages in turn, each with
 // sums of its own, which meet in LDS at the end.  S^T = K Q^T and O^T = V^T P^T, so that a lane holds one row's scores and probabilities.  Codes go from memory to
 // registers to the matrix units; a page's values are on their way while its scores are made, the next page's keys while its values are used.
 // Memory bound: 2 * D bytes a token and head.
-template <int DT, int DP>
-__global__ __launch_bounds__(256, DP <= 160 || (DP == 192 && DT == 1) ? 2 : 1) void kv_split_kernel(KvAttendArgs a)
+template <int DT, int DP, int QT>
+__global__ __launch_bounds__(256, (QT == 1 && DP <= 160) || (QT == 1 && DP == 192 && DT == 1) || (QT == 2 && DP * (DT == 1 ? 1 : 2) <= 128) ? 2 : 1) void kv_split_kernel(KvAttendArgs a)
 {
     constexpr int KS = DP / 32, DTL = DP / 16, NQ = QParts<DT>::N, NP = QParts<DT>::NP, NB = QParts<DT>::NB;
     constexpr int LDO = DP + 4;
     __shared__ __align__(16) float xo[4][16][LDO];
-    __shared__ float2 xml[4][16];
-    __shared__ float2 xw[kMassPages * 16];               // a page's sums of weights under a maximum, where all of them are here
+    __shared__ float2 xml[4][16 * QT];
+    __shared__ float2 xw[QT == 1 ? kMassPages * 16 : 1];               // a page's sums of weights under a maximum, where all of them are here
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 15, gq = lane >> 4;
-    const int row_tiles = (a.rows_pad + 15) / 16;
+    constexpr int TR = 16 * QT;                          // rows of the tile
+    const int row_tiles = (a.rows_pad + TR - 1) / TR;
     const int split = blockIdx.x % a.splits, rt = (blockIdx.x / a.splits) % row_tiles, bg = blockIdx.x / a.splits / row_tiles;
     const int b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
-    const bool own_mass = a.mass && a.splits == 1 && row_tiles == 1 && a.kv.max_pages <= kMassPages;
+    const bool own_mass = QT == 1 && a.mass && a.splits == 1 && row_tiles == 1 && a.kv.max_pages <= kMassPages;
     // places of this wavefront's pages: those of the next 64 lie in the lanes.  Where the first is known before the length, they are asked for at once
     // (a workgroup starts with a chain of dependent loads, 1 us each under load: length, place, codes)
     const int32_t* const table = a.kv.table + (int64_t)b * a.kv.max_pages;
@@ -115,39 +116,53 @@ __global__ __launch_bounds__(256, DP <= 160 || (DP == 192 && DT == 1) ? 2 : 1) v
     const int n_all = s.n;
     s.n = s.n < a.max_new ? s.n : a.max_new;
     const int rows = s.n * a.R;
-    if (rt * 16 >= rows || rows > kSplitRows) return;
-    const int rr = rt * 16 + c, qi = rr / a.R, qh = g * a.R + rr % a.R;
-    const bool live = rr < rows;
-    const int lim = !live ? 0 : a.causal ? s.len - n_all + qi + 1 : s.len;             // tokens that the row sees
-    const int last_row = min(rows, rt * 16 + 16) - 1;
+    if (rt * TR >= rows || rows > kSplitRows) return;
+    int lim[QT];                                         // tokens that the lane's rows see
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+        const int rr = rt * TR + x * 16 + c;
+        lim[x] = rr >= rows ? 0 : a.causal ? s.len - n_all + rr / a.R + 1 : s.len;
+    }
+    const int last_row = min(rows, rt * TR + TR) - 1;
     const int most = a.causal ? max(0, s.len - n_all + last_row / a.R + 1) : s.len;
-    const int least = a.causal ? s.len - n_all + (rt * 16) / a.R + 1 : s.len;          // every row of the tile sees as many
+    const int least = a.causal ? s.len - n_all + (rt * TR) / a.R + 1 : s.len;          // every row of the tile sees as many
     const int full = s.len / kPage, units = (most + kPage - 1) / kPage;
     const int per = (units + a.splits - 1) / a.splits, u0 = split * per, u1 = min(units, u0 + per);
-    const int64_t slot0 = ((int64_t)bg * a.rows_pad + rt * 16) * a.splits + split;      // of the tile's first row
+    const int64_t slot0 = ((int64_t)bg * a.rows_pad + rt * TR) * a.splits + split;      // of the tile's first row
     if (u0 >= u1 && a.splits > 1) {
-        if (tid < 16 && rt * 16 + tid < rows) a.part_ml[slot0 + (int64_t)tid * a.splits] = float2{-__builtin_inff(), 0.0f};
+        if (tid < TR && rt * TR + tid < rows) a.part_ml[slot0 + (int64_t)tid * a.splits] = float2{-__builtin_inff(), 0.0f};
         return;
     }
 
-    bf16x8 q[NQ][KS];
+    bf16x8 q[QT][NQ][KS];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-        bf16x8 p[NQ];
-        const int d = k * 32 + gq * 8;
-        if (live && d < D) QParts<DT>::load(a, (s.first + qi) * a.q_token + qh * a.q_head + d, p);
+    for (int x = 0; x < QT; ++x) {
+        const int rr = rt * TR + x * 16 + c;
+        const bool live = rr < rows;
+        const int64_t at = (s.first + (live ? rr / a.R : 0)) * a.q_token + (g * a.R + rr % a.R) * a.q_head;
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) q[i][k] = live && d < D ? p[i] : bf16x8{};
+        for (int k = 0; k < KS; ++k) {
+            bf16x8 p[NQ];
+            const int d = k * 32 + gq * 8;
+            if (live && d < D) QParts<DT>::load(a, at + d, p);
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) q[x][i][k] = live && d < D ? p[i] : bf16x8{};
+        }
     }
 
-    float m = -__builtin_inff(), l = 0.0f;               // of the lane's row; l: of the lane's own tokens
-    f32x4 o[DTL];
+    float m[QT], l[QT];                                  // of the lane's rows; l: of the lane's own tokens
+    f32x4 o[QT][DTL];
 #pragma unroll
-    for (int t = 0; t < DTL; ++t) o[t] = f32x4{0, 0, 0, 0};
+    for (int x = 0; x < QT; ++x) {
+        m[x] = -__builtin_inff();
+        l[x] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < DTL; ++t) o[x][t] = f32x4{0, 0, 0, 0};
+    }
     float2* const page_w = a.page_w + (int64_t)bg * a.kv.max_pages * a.rows_pad;
 
     // scores of a page -> probabilities (times 2^13), the running maximum and sum; returns what the sums so far are to be multiplied by
-    auto softmax = [&](f32x4* sc, float factor, int u) {
+    auto softmax = [&](int x, f32x4* sc, float factor, int u) {
         const int base = u * kPage;
         float mx = -__builtin_inff();
         if (base + kPage <= least) {
@@ -160,26 +175,27 @@ __global__ __launch_bounds__(256, DP <= 160 || (DP == 192 && DT == 1) ? 2 : 1) v
             for (int T = 0; T < 4; ++T)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    sc[T][r] = base + T * 16 + gq * 4 + r < lim ? sc[T][r] * factor : -__builtin_inff();
+                    sc[T][r] = base + T * 16 + gq * 4 + r < lim[x] ? sc[T][r] * factor : -__builtin_inff();
                     mx = fmaxf(mx, sc[T][r]);
                 }
         }
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float mn = fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.0f : mn;
-        const float alpha = exp2_of(m - ms), off = kPBias - ms;
+        const float mn = fmaxf(m[x], mx), ms = mn == -__builtin_inff() ? 0.0f : mn;
+        const float alpha = exp2_of(m[x] - ms), off = kPBias - ms;
         float sum = 0.0f;
 #pragma unroll
         for (int T = 0; T < 4; ++T)
 #pragma unroll
             for (int r = 0; r < 4; ++r) { sc[T][r] = exp2_of(sc[T][r] + off); sum += sc[T][r]; }
-        m = mn;
-        l = __builtin_fmaf(l, alpha, sum);
+        m[x] = mn;
+        l[x] = __builtin_fmaf(l[x], alpha, sum);
         if (a.mass) {
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
-            if (gq == 0 && live) {
-                if (own_mass) xw[u * 16 + c] = float2{ms, sum};
+            const int rr = rt * TR + x * 16 + c;
+            if (gq == 0 && rr < rows) {
+                if (QT == 1 && own_mass) xw[u * 16 + c] = float2{ms, sum};
                 else page_w[(int64_t)u * a.rows_pad + rr] = float2{ms, sum};
             }
         }
@@ -220,9 +236,11 @@ __global__ __launch_bounds__(256, DP <= 160 || (DP == 192 && DT == 1) ? 2 : 1) v
         const float ks = __uint_as_float(bcast(__float_as_uint(my_ks), it & 63)) * a.scale, vs = __uint_as_float(bcast(__float_as_uint(my_vs), it & 63));
 #pragma unroll
         for (int i = 0; i < DTL; ++i) vb[i] = rec[(2 * KS + i) * 64];
-        f32x4 sc[4];
+        f32x4 sc[QT][4];
 #pragma unroll
-        for (int T = 0; T < 4; ++T) sc[T] = f32x4{0, 0, 0, 0};
+        for (int x = 0; x < QT; ++x)
+#pragma unroll
+            for (int T = 0; T < 4; ++T) sc[x][T] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int T2 = 0; T2 < 2; ++T2)
 #pragma unroll
@@ -230,10 +248,12 @@ __global__ __launch_bounds__(256, DP <= 160 || (DP == 192 && DT == 1) ? 2 : 1) v
                 const uint4 w = kb[T2 * KS + k];
                 const bf16x8 k0 = codes_bf16(w.x, w.y), k1 = codes_bf16(w.z, w.w);
 #pragma unroll
-                for (int i = 0; i < NQ; ++i) {
-                    sc[2 * T2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[i][k], sc[2 * T2], 0, 0, 0);
-                    sc[2 * T2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][k], sc[2 * T2 + 1], 0, 0, 0);
-                }
+                for (int x = 0; x < QT; ++x)
+#pragma unroll
+                    for (int i = 0; i < NQ; ++i) {
+                        sc[x][2 * T2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[x][i][k], sc[x][2 * T2], 0, 0, 0);
+                        sc[x][2 * T2 + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[x][i][k], sc[x][2 * T2 + 1], 0, 0, 0);
+                    }
             }
         if (u + 4 < ufull) {
             if ((it & 63) == 63) fetch(u + 4, false);
@@ -241,87 +261,100 @@ __global__ __launch_bounds__(256, DP <= 160 || (DP == 192 && DT == 1) ? 2 : 1) v
 #pragma unroll
             for (int i = 0; i < 2 * KS; ++i) kb[i] = rec[i * 64];
         }
-        const float alpha = softmax(sc, ks, u);
-        f16x8 p[NP][2];
+        float alpha[QT];
+        f16x8 p[QT][NP][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int x = 0; x < QT; ++x) {
+            alpha[x] = softmax(x, sc[x], ks, u);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float f = sc[2 * h + (j >> 2)][j & 3];
-                const _Float16 hi = (_Float16)f;
-                p[0][h][j] = hi;
-                if constexpr (NP > 1) p[1][h][j] = (_Float16)(f - (float)hi);
-            }
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float f = sc[x][2 * h + (j >> 2)][j & 3];
+                    const _Float16 hi = (_Float16)f;
+                    p[x][0][h][j] = hi;
+                    if constexpr (NP > 1) p[x][1][h][j] = (_Float16)(f - (float)hi);
+                }
+        }
 #pragma unroll
         for (int t = 0; t < DTL; ++t) {
             const f16x8 v0 = f16_of(codes_f16(vb[t].x), codes_f16(vb[t].y)), v1 = f16_of(codes_f16(vb[t].z), codes_f16(vb[t].w));
-            f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[i][0], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[i][1], acc, 0, 0, 0);
+            for (int x = 0; x < QT; ++x) {
+                f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[x][i][0], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[x][i][1], acc, 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[x][t][r] = __builtin_fmaf(acc[r], vs, o[x][t][r] * alpha[x]);
             }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[t][r] = __builtin_fmaf(acc[r], vs, o[t][r] * alpha);
         }
     }
     if (u < u1 && u == full) {                           // the tail, as the last page
         const int count = s.len - full * kPage;
         const uint16_t* tk = a.kv.tails + kv_tail(a.kv, b, g);
         const uint16_t* tv = tk + kPage * DP;
-        f32x4 sc[4];
 #pragma unroll
-        for (int T = 0; T < 4; ++T) {
-            sc[T] = f32x4{0, 0, 0, 0};
-            if (T * 16 < count) {
+        for (int x = 0; x < QT; ++x) {
+            f32x4 sc[4];
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const bf16x8 w = bf16_of(*(const uint4*)(tk + (T * 16 + c) * DP + k * 32 + gq * 8));
+            for (int T = 0; T < 4; ++T) {
+                sc[T] = f32x4{0, 0, 0, 0};
+                if (T * 16 < count) {
 #pragma unroll
-                    for (int i = 0; i < NQ; ++i) sc[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, q[i][k], sc[T], 0, 0, 0);
+                    for (int k = 0; k < KS; ++k) {
+                        const bf16x8 w = bf16_of(*(const uint4*)(tk + (T * 16 + c) * DP + k * 32 + gq * 8));
+#pragma unroll
+                        for (int i = 0; i < NQ; ++i) sc[T] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, q[x][i][k], sc[T], 0, 0, 0);
+                    }
                 }
             }
-        }
-        const float alpha = softmax(sc, a.scale, u);
-        bf16x8 p[NB][2];
+            const float alpha = softmax(x, sc, a.scale, u);
+            bf16x8 p[NB][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float f = sc[2 * h + (j >> 2)][j & 3];
+                for (int j = 0; j < 8; ++j) {
+                    float f = sc[2 * h + (j >> 2)][j & 3];
 #pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    p[i][h][j] = (__bf16)f;
-                    f -= (float)p[i][h][j];
+                    for (int i = 0; i < NB; ++i) {
+                        p[i][h][j] = (__bf16)f;
+                        f -= (float)p[i][h][j];
+                    }
                 }
-            }
 #pragma unroll
-        for (int t = 0; t < DTL; ++t) {
+            for (int t = 0; t < DTL; ++t) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[t][r] *= alpha;
+                for (int r = 0; r < 4; ++r) o[x][t][r] *= alpha;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                u32 w[4];
+                for (int h = 0; h < 2; ++h) {
+                    u32 w[4];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {            // four tokens of an element; those behind the last are whatever the memory held
-                    const int t0 = (2 * h + e) * 16 + gq * 4;
-                    uint2 r = {0, 0};
-                    if (t0 < count) r = *(const uint2*)(tv + ((t0 >> 2) * DP + t * 16 + c) * 4);
-                    const int left = count - t0;
-                    w[2 * e] = left >= 2 ? r.x : left == 1 ? r.x & 0xFFFFu : 0u;
-                    w[2 * e + 1] = left >= 4 ? r.y : left == 3 ? r.y & 0xFFFFu : 0u;
+                    for (int e = 0; e < 2; ++e) {        // four tokens of an element; those behind the last are whatever the memory held
+                        const int t0 = (2 * h + e) * 16 + gq * 4;
+                        uint2 r = {0, 0};
+                        if (t0 < count) r = *(const uint2*)(tv + ((t0 >> 2) * DP + t * 16 + c) * 4);
+                        const int left = count - t0;
+                        w[2 * e] = left >= 2 ? r.x : left == 1 ? r.x & 0xFFFFu : 0u;
+                        w[2 * e + 1] = left >= 4 ? r.y : left == 3 ? r.y & 0xFFFFu : 0u;
+                    }
+                    const bf16x8 v = bf16_of(uint4{w[0], w[1], w[2], w[3]});
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) o[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[i][h], o[x][t], 0, 0, 0);
                 }
-                const bf16x8 v = bf16_of(uint4{w[0], w[1], w[2], w[3]});
-#pragma unroll
-                for (int i = 0; i < NB; ++i) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[i][h], o[t], 0, 0, 0);
             }
         }
     }
 
     // the four wavefronts' sums under one maximum
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (gq == 0) xml[wid][c] = float2{m, l};
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+        l[x] += __shfl_xor(l[x], 16);
+        l[x] += __shfl_xor(l[x], 32);
+        if (gq == 0) xml[wid][x * 16 + c] = float2{m[x], l[x]};
+    }
     __syncthreads();
     auto total = [&](int r) {                            // (maximum, sum) of a row of the tile
         const float M = fmaxf(fmaxf(xml[0][r].x, xml[1][r].x), fmaxf(xml[2][r].x, xml[3][r].x)), Ms = M == -__builtin_inff() ? 0.0f : M;
@@ -330,38 +363,39 @@ __global__ __launch_bounds__(256, DP <= 160 || (DP == 192 && DT == 1) ? 2 : 1) v
         for (int w = 0; w < 4; ++w) L += xml[w][r].y * exp2_of(xml[w][r].x - Ms);
         return float2{M, L};
     };
-    {
-        const float M = total(c).x, f = exp2_of(m - (M == -__builtin_inff() ? 0.0f : M));
 #pragma unroll
-        for (int t = 0; t < DTL; ++t) *(f32x4*)&xo[wid][c][t * 16 + gq * 4] = o[t] * f;
-    }
-    __syncthreads();
-    for (int i = tid; i < 16 * (DP / 4); i += 256) {
-        const int r = i / (DP / 4), d = i % (DP / 4) * 4;
-        if (rt * 16 + r >= rows || d >= D) continue;
-        f32x4 v = *(const f32x4*)&xo[0][r][d];
+    for (int x = 0; x < QT; ++x) {
+        const float M = total(x * 16 + c).x, f = exp2_of(m[x] - (M == -__builtin_inff() ? 0.0f : M));
+        if (x) __syncthreads();
 #pragma unroll
-        for (int w = 1; w < 4; ++w) v += *(const f32x4*)&xo[w][r][d];
-        if (a.splits > 1) {
-            *(f32x4*)(a.part_o + (slot0 + (int64_t)r * a.splits) * DP + d) = v;
-        } else {
-            const float L = total(r).y;
-            const int rw = rt * 16 + r;
-            store4<DT>(a.out, ((s.first + rw / a.R) * a.H + g * a.R + rw % a.R) * (int64_t)D + d, v * (L == 0.0f ? 0.0f : 1.0f / L));
+        for (int t = 0; t < DTL; ++t) *(f32x4*)&xo[wid][c][t * 16 + gq * 4] = o[x][t] * f;
+        __syncthreads();
+        for (int i = tid; i < 16 * (DP / 4); i += 256) {
+            const int r = i / (DP / 4), d = i % (DP / 4) * 4, rw = rt * TR + x * 16 + r;
+            if (rw >= rows || d >= D) continue;
+            f32x4 v = *(const f32x4*)&xo[0][r][d];
+#pragma unroll
+            for (int w = 1; w < 4; ++w) v += *(const f32x4*)&xo[w][r][d];
+            if (a.splits > 1) {
+                *(f32x4*)(a.part_o + (slot0 + (int64_t)(x * 16 + r) * a.splits) * DP + d) = v;
+            } else {
+                const float L = total(x * 16 + r).y;
+                store4<DT>(a.out, ((s.first + rw / a.R) * a.H + g * a.R + rw % a.R) * (int64_t)D + d, v * (L == 0.0f ? 0.0f : 1.0f / L));
+            }
         }
     }
-    if (tid < 16 && rt * 16 + tid < rows) {
+    if (tid < TR && rt * TR + tid < rows) {
         const float2 ml = total(tid);
-        const int rw = rt * 16 + tid;
+        const int rw = rt * TR + tid;
         if (a.splits > 1 || (a.mass && !own_mass)) a.part_ml[slot0 + (int64_t)tid * a.splits] = ml;
         if (a.splits == 1 && a.lse) a.lse[(s.first + rw / a.R) * a.H + g * a.R + rw % a.R] = ml.y == 0.0f ? -__builtin_inff() : (ml.x - kPBias + __log2f(ml.y)) * kLn2;
     }
-    if (own_mass) {                                      // sixteen lanes a page
+    if (QT == 1 && own_mass) {                           // sixteen lanes a page
         const float2 ml = total(c);
         const int pages = (s.len + kPage - 1) / kPage;
         for (int p = tid >> 4; p < pages; p += 16) {
             float sum = 0.0f;
-            if (p < units && live) {
+            if (p < units && c < rows) {
                 const float2 w = xw[p * 16 + c];
                 if (w.y != 0.0f) sum = w.y * exp2_of(w.x - ml.x) / ml.y;
             }
@@ -393,7 +427,7 @@ __device__ inline float2 kv_row_total(const float2* ml, int splits, int lane)
 // the rows' sums are known, a workgroup per 256 pages.  A row's parts are read by all four wavefronts at once, several parts a load: with one wavefront a row, part
 // after part, 64 parts took 64 us instead of 5.
 template <int DT, int DP>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_blocks, int page_blocks)
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_blocks, int page_blocks, int tile_rows)
 {
     constexpr int LPP = DP / 4, PPW = kWave / LPP;       // lanes a part, parts a load (a part of more than 32 elements of four: one)
     __shared__ float2 xml[kSplitRows];
@@ -454,7 +488,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_bl
         float sum = 0.0f;
         for (int r = 0; r < rows; ++r) {
             // a row's tile came to the pages that the tile's last row sees some token of
-            const int top = a.causal ? s.len - n_all + min(rows - 1, r | 15) / a.R + 1 : s.len;
+            const int top = a.causal ? s.len - n_all + min(rows - 1, r | (tile_rows - 1)) / a.R + 1 : s.len;
             if (p * kPage >= top || w[r].y == 0.0f) continue;
             sum += w[r].y * exp2_of(w[r].x - xml[r].x) * xml[r].y;
         }

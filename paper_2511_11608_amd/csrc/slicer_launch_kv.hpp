@@ -15,8 +15,12 @@ inline dim3 kv_grid(int64_t blocks, int64_t pairs)
     return dim3((unsigned)blocks, (unsigned)y, (unsigned)((pairs + y - 1) / y));
 }
 
+// Head sizes up to this one have registers for 32 rows at a time; larger ones (fp32 queries) would spill.
+constexpr int kWideTile = 160;
+
 struct KvAttendLaunch {
-    int split_tiles;          // row tiles of sixteen for the sequences that are split; 0: none can be
+    int tile_rows;            // rows of a tile of the sequences that are split: 16 or 32
+    int split_tiles;          // their tiles
     int row_blocks, page_blocks;
     int prompt_tiles;         // row tiles of 128; 0: no sequence can have that many rows
     int mass_tiles;           // four pages each
@@ -67,10 +71,12 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, const KvAttendLaunch& p, hipS
     const unsigned pairs = (unsigned)(a.kv.seqs * a.kv.G);
     kv_by_size(a.kv.dp, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        if (p.split_tiles) {
-            hipLaunchKernelGGL((kv_split_kernel<DT, DP>), dim3(pairs * (unsigned)(p.split_tiles * a.splits)), dim3(256), 0, st, a);
+        {
+            const dim3 grid(pairs * (unsigned)(p.split_tiles * a.splits));
+            if (p.tile_rows == 16) hipLaunchKernelGGL((kv_split_kernel<DT, DP, 1>), grid, dim3(256), 0, st, a);
+            else if constexpr (DP <= kWideTile) hipLaunchKernelGGL((kv_split_kernel<DT, DP, 2>), grid, dim3(256), 0, st, a);
             if (p.row_blocks + p.page_blocks)
-                hipLaunchKernelGGL((kv_join_kernel<DT, DP>), dim3(pairs * (unsigned)(p.row_blocks + p.page_blocks)), dim3(256), 0, st, a, p.row_blocks, p.page_blocks);
+                hipLaunchKernelGGL((kv_join_kernel<DT, DP>), dim3(pairs * (unsigned)(p.row_blocks + p.page_blocks)), dim3(256), 0, st, a, p.row_blocks, p.page_blocks, p.tile_rows);
         }
         if (p.prompt_tiles) {
             hipLaunchKernelGGL((kv_prompt_kernel<DT, DP>), dim3(pairs * (unsigned)p.prompt_tiles), dim3(256), 0, st, a, p.prompt_tiles);
