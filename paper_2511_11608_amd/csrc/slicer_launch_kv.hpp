@@ -60,7 +60,7 @@ template <int DT>
 hipError_t launch_kv_read(const KvReadArgs& a, int64_t blocks, hipStream_t st)
 {
     kv_by_size(a.kv.dp, [&](auto dp) {
-        hipLaunchKernelGGL((kv_read_kernel<DT, decltype(dp)::value>), kv_grid(blocks, (int64_t)a.kv.seqs * a.kv.G), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((kv_read_kernel<DT, decltype(dp)::value>), kv_grid(2 * blocks, (int64_t)a.kv.seqs * a.kv.G), dim3(256), 0, st, a);
     });
     return hipGetLastError();
 }
