@@ -96,7 +96,7 @@ def load() -> C.CDLL:
         L.slicer_kv_append.restype = cint
         L.slicer_kv_append.argtypes = [kvp, vp, vp, cint, i64, vp, cint, i64, i64, i64, i64, vp]
         L.slicer_kv_attend_sizes.restype = cint
-        L.slicer_kv_attend_sizes.argtypes = [kvp, cint, i64, cint, i64, szp]
+        L.slicer_kv_attend_sizes.argtypes = [kvp, cint, i64, cint, i64, cint, szp]
         L.slicer_kv_attend.restype = cint
         L.slicer_kv_attend.argtypes = [kvp, vp, cint, cint, i64, vp, cint, i64, i64, i64, dbl, cint, vp, vp, vp, dbl, vp, vp]
         L.slicer_kv_read.restype = cint
@@ -444,15 +444,15 @@ def slicer_kv_append(kv: KvCache, k: torch.Tensor, v: torch.Tensor, starts: torc
                                                        k.stride(0), k.stride(1), v.stride(0), v.stride(1), _stream_handle(stream)))
 
 
-def slicer_kv_attend_sizes(kv: KvCache, heads: int, tokens: int, max_new: int, max_len: int) -> int:
-    """Workspace bytes of slicer_kv_attend."""
+def slicer_kv_attend_sizes(kv: KvCache, heads: int, tokens: int, max_new: int, max_len: int, with_mass: bool = True) -> int:
+    """Workspace bytes of slicer_kv_attend, with `mass` or without."""
     w = C.c_size_t(0)
-    _check("slicer_kv_attend_sizes", load().slicer_kv_attend_sizes(C.byref(kv.c()), heads, tokens, max_new, max_len, C.byref(w)))
+    _check("slicer_kv_attend_sizes", load().slicer_kv_attend_sizes(C.byref(kv.c()), heads, tokens, max_new, max_len, int(with_mass), C.byref(w)))
     return w.value
 
 
-def alloc_kv_workspace(kv: KvCache, heads: int, tokens: int, max_new: int, max_len: int) -> torch.Tensor:
-    return torch.empty(max(slicer_kv_attend_sizes(kv, heads, tokens, max_new, max_len), 256), dtype=torch.uint8, device=kv.pages.device)
+def alloc_kv_workspace(kv: KvCache, heads: int, tokens: int, max_new: int, max_len: int, with_mass: bool = True) -> torch.Tensor:
+    return torch.empty(max(slicer_kv_attend_sizes(kv, heads, tokens, max_new, max_len, with_mass), 256), dtype=torch.uint8, device=kv.pages.device)
 
 
 def slicer_kv_attend(kv: KvCache, q: torch.Tensor, starts: torch.Tensor, max_new: int, max_len: int, scale: float, out: torch.Tensor,
@@ -469,7 +469,7 @@ def slicer_kv_attend(kv: KvCache, q: torch.Tensor, starts: torch.Tensor, max_new
         _kv_tensor("mass", mass, torch.float32, (kv.seqs, kv.kv_heads, kv.max_pages))
     L = load()
     need = C.c_size_t(0)
-    _check("slicer_kv_attend_sizes", L.slicer_kv_attend_sizes(C.byref(c), heads, tokens, max_new, max_len, C.byref(need)))
+    _check("slicer_kv_attend_sizes", L.slicer_kv_attend_sizes(C.byref(c), heads, tokens, max_new, max_len, int(mass is not None), C.byref(need)))
     if not workspace.is_cuda or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need.value:
         raise ValueError(f"workspace must be a contiguous tensor of {need.value} bytes on the GPU")
     _kv_devices(kv, out, lse, mass, workspace)

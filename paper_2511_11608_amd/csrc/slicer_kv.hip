@@ -65,10 +65,10 @@ inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 struct AttendPlan {
     int splits, rows_pad;
     KvAttendLaunch launch;
-    size_t off_part_ml, off_part_o, off_page_w, off_row_ml, total;
+    size_t off_part_ml, off_part_o, off_page_w, off_row_w, off_tile_mass, total;
 };
 
-AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_new, int64_t max_len)
+AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_new, int64_t max_len, bool mass)
 {
     AttendPlan p;
     const int64_t pairs = (int64_t)kv->seqs * kv->kv_heads, R = heads / kv->kv_heads;
@@ -81,15 +81,19 @@ AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_n
     const int64_t tiles = pairs * p.launch.split_tiles;
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((512 + tiles - 1) / tiles, (pages + 3) / 4));
     p.launch.row_blocks = p.splits > 1 ? p.rows_pad : 0;
-    p.launch.page_blocks = p.splits > 1 || p.rows_pad > 16 || kv->max_pages > kMassPages ? (int)((pages + 255) / 256) : 0;
+    p.launch.page_blocks = mass && (p.splits > 1 || p.rows_pad > 16 || kv->max_pages > kMassPages) ? (int)((pages + 255) / 256) : 0;
     p.launch.prompt_tiles = rows > kSplitRows ? (int)((rows + kTileRows - 1) / kTileRows) : 0;
-    p.launch.mass_tiles = (int)((pages + 3) / 4);
+    p.launch.mass_blocks = mass && p.launch.prompt_tiles ? (int)((pages + 255) / 256) : 0;
+    // Two workgroups a CU, which have 1 KB a page each to keep a tile's weights in: at most 512 of them, and no more than 2 GB together where half are enough.
+    const size_t slot = (size_t)kv->max_pages * kTileRows * sizeof(float2);
+    p.launch.prompt_slots = p.launch.mass_blocks ? (int)std::min<int64_t>(pairs * p.launch.prompt_tiles, slot * 512 <= (size_t)2 << 30 ? 512 : 256) : 0;
     size_t o = 0;
     const size_t slots = (size_t)pairs * p.rows_pad * p.splits;
     p.off_part_ml = o; o += align256(slots * sizeof(float2));
     p.off_part_o = o; o += align256(p.splits > 1 ? slots * round32(kv->head_dim) * sizeof(float) : 0);
-    p.off_page_w = o; o += align256((size_t)pairs * kv->max_pages * p.rows_pad * sizeof(float2));
-    p.off_row_ml = o; o += align256(p.launch.prompt_tiles ? (size_t)tokens * heads * sizeof(float2) : 0);
+    p.off_page_w = o; o += align256(mass ? (size_t)pairs * kv->max_pages * p.rows_pad * sizeof(float2) : 0);
+    p.off_row_w = o; o += align256(slot * p.launch.prompt_slots);
+    p.off_tile_mass = o; o += align256(p.launch.mass_blocks ? (size_t)pairs * p.launch.prompt_tiles * kv->max_pages * sizeof(float) : 0);
     p.total = o;
     return p;
 }
@@ -133,12 +137,12 @@ int slicer_kv_append(const slicer_kv* kv, const void* k, const void* v, slicer_d
     return fail(dt == SLICER_F32 ? launch_kv_append<0>(a, blocks, (hipStream_t)hip_stream) : launch_kv_append<1>(a, blocks, (hipStream_t)hip_stream));
 }
 
-int slicer_kv_attend_sizes(const slicer_kv* kv, int heads, int64_t tokens, int max_new, int64_t max_len, size_t* workspace_bytes)
+int slicer_kv_attend_sizes(const slicer_kv* kv, int heads, int64_t tokens, int max_new, int64_t max_len, int with_mass, size_t* workspace_bytes)
 {
     int rc = check_kv(kv);
     if (rc) return rc;
     if (heads < 1 || heads % kv->kv_heads || tokens < 0 || tokens >= (int64_t)1 << 31 || (tokens > 0 && max_new < 1) || max_len < 0) return SLICER_EINVAL;
-    if (workspace_bytes) *workspace_bytes = tokens ? plan_attend(kv, heads, tokens, max_new, max_len).total : 0;
+    if (workspace_bytes) *workspace_bytes = tokens ? plan_attend(kv, heads, tokens, max_new, max_len, with_mass != 0).total : 0;
     return SLICER_OK;
 }
 
@@ -151,10 +155,9 @@ int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int he
     if (heads < 1 || heads % kv->kv_heads || !std::isfinite(scale) || !(mass_decay >= 0.0 && mass_decay <= 1.0) || max_len < 0) return SLICER_EINVAL;
     if (tokens == 0) return SLICER_OK;
     if (!q || !out || !workspace) return SLICER_EINVAL;
-    AttendPlan p = plan_attend(kv, heads, tokens, max_new, max_len);
+    const AttendPlan p = plan_attend(kv, heads, tokens, max_new, max_len, mass != nullptr);
     const int64_t pairs = (int64_t)kv->seqs * kv->kv_heads;
-    if (!mass) p.launch.page_blocks = p.launch.mass_tiles = 0;
-    for (int64_t n : {(int64_t)p.launch.split_tiles * p.splits, (int64_t)p.launch.row_blocks + p.launch.page_blocks, (int64_t)p.launch.prompt_tiles, (int64_t)p.launch.mass_tiles})
+    for (int64_t n : {(int64_t)p.launch.split_tiles * p.splits, (int64_t)p.launch.row_blocks + p.launch.page_blocks, (int64_t)p.launch.prompt_tiles, (int64_t)p.launch.mass_blocks})
         if (pairs * n >= (int64_t)1 << 31) return SLICER_EINVAL;        // more workgroups than a launch can have
     KvAttendArgs a;
     a.kv = view_of(kv);
@@ -167,7 +170,8 @@ int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int he
     a.H = heads;
     a.max_new = max_new;
     a.causal = causal != 0;
-    a.scale = (float)(scale * 1.44269504088896340736);
+    a.scale = (float)(std::fabs(scale) * 1.44269504088896340736);
+    a.flip = scale < 0.0;
     a.out = out;
     a.lse = lse;
     a.mass = mass;
@@ -179,7 +183,8 @@ int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int he
     a.part_ml = (float2*)(ws + p.off_part_ml);
     a.part_o = (float*)(ws + p.off_part_o);
     a.page_w = (float2*)(ws + p.off_page_w);
-    a.row_ml = (float2*)(ws + p.off_row_ml);
+    a.row_w = (float2*)(ws + p.off_row_w);
+    a.tile_mass = (float*)(ws + p.off_tile_mass);
     return fail(dt == SLICER_F32 ? launch_kv_attend<0>(a, p.launch, (hipStream_t)hip_stream) : launch_kv_attend<1>(a, p.launch, (hipStream_t)hip_stream));
 }
 

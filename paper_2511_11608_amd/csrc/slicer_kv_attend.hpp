@@ -26,7 +26,8 @@ struct KvAttendArgs {
     const int32_t* starts;
     int64_t tokens;
     int R, H, max_new, causal;
-    float scale;                  // of the scores, times log2(e)
+    float scale;                  // of the scores, times log2(e); not negative
+    int flip;                     // queries are negated instead
     void* out;                    // [tokens][H][D]
     float* lse;                   // [tokens][H] or null
     float* mass;                  // [seqs][G][max_pages] or null
@@ -37,7 +38,9 @@ struct KvAttendArgs {
     float2* part_ml;
     float* part_o;
     float2* page_w;               // [sequence, head][max_pages][rows_pad] a page's sum of weights under a maximum
-    float2* row_ml;               // [tokens][H] (maximum, 1 / sum) of the rows that are not split
+    // rows that are not split, with weights: [workgroup][max_pages][128] a page's sum of a tile's rows, and [sequence, head][tiles][max_pages] of the tile
+    float2* row_w;
+    float* tile_mass;
 };
 
 // queries -> bf16 operands: element j of part i
@@ -48,7 +51,16 @@ struct QParts<1> {
     static constexpr int N = 1;
     static constexpr int NP = 1;          // fp16 numbers a probability is held in
     static constexpr int NB = 2;          // bf16 numbers
-    __device__ static inline void load(const KvAttendArgs& a, int64_t at, bf16x8* p) { p[0] = bf16_of(Row8<1>::bf16(a.q, at, a.wide_q)); }
+    __device__ static inline void load(const KvAttendArgs& a, int64_t at, bf16x8* p)
+    {
+        uint4 w = Row8<1>::bf16(a.q, at, a.wide_q);
+        const u32 sign = a.flip ? 0x80008000u : 0u;
+        w.x ^= sign;
+        w.y ^= sign;
+        w.z ^= sign;
+        w.w ^= sign;
+        p[0] = bf16_of(w);
+    }
 };
 template <>
 struct QParts<0> {
@@ -61,6 +73,7 @@ struct QParts<0> {
         Row8<0>::f32(a.q, at, a.wide_q, f);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
+            if (a.flip) f[j] = -f[j];
             const __bf16 h = (__bf16)f[j];
             const float r = f[j] - (float)h;
             const __bf16 m = (__bf16)r;
@@ -558,325 +571,293 @@ __device__ inline void stage_tail(uint16_t* keys, uint16_t* values, const uint16
     }
 }
 
+// Probabilities are held times 2^8 here: a row's maximum may grow by 2^6 before its sums are scaled down to it (nearly every page raises the
+// maximum of some row, hardly any by that much), and a page's value scale may be twice the one that outputs are held in: 2^15 at most in fp16.
+constexpr float kPromptBias = 8.0f, kSlack = 6.0f;
+
+__device__ inline float other_half(float x, float* mine)             // the values of lanes l and l + 32 of a pair, in both of them
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    *mine = __uint_as_float(r[0]);
+    return __uint_as_float(r[1]);
+}
+
+// `slots`: workgroups that hold weights of a tile's rows by page on the way (a.mass), each in a part of page_w of its own.
 template <int DT, int DP>
-__global__ __launch_bounds__(256, 1) void kv_prompt_kernel(KvAttendArgs a, int row_tiles)
+__global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv_prompt_kernel(KvAttendArgs a, int row_tiles)
 {
     constexpr int KK = DP / 16, DL = DP / 32, NQ = QParts<DT>::N, NP = QParts<DT>::NP, NB = QParts<DT>::NB;
     constexpr int NR = (4 * DP + 255) / 256;             // records of keys (and of values) a thread
-    __shared__ __align__(16) uint16_t x[2][PromptTile<DP>::kAll];
+    __shared__ __align__(16) uint16_t buf[2][PromptTile<DP>::kAll];
+    __shared__ float2 xrow[kTileRows];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 31, h = lane >> 5;
-    // the longest tiles first; a head's tiles on one XCD (workgroup i runs on XCD i % 8), whose L2 its pages then are in
-    const int heads = a.kv.seqs * a.kv.G, bg = blockIdx.x % heads, rt = row_tiles - 1 - (int)(blockIdx.x / heads);
-    const int b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
-    KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
-    const int n_all = s.n;
-    s.n = s.n < a.max_new ? s.n : a.max_new;
-    const int64_t rows = (int64_t)s.n * a.R;
-    if (rows <= kSplitRows || (int64_t)rt * kTileRows >= rows) return;
-    const int64_t rr = (int64_t)rt * kTileRows + wid * 32 + c;
-    const bool live = rr < rows;
-    const int qi = (int)((live ? rr : rows - 1) / a.R), qh = g * a.R + (int)((live ? rr : rows - 1) % a.R);
-    const int lim = !live ? 0 : a.causal ? s.len - n_all + qi + 1 : s.len;
-    const int64_t last_row = min(rows, (int64_t)(rt + 1) * kTileRows) - 1;
-    const int most = a.causal ? max(0, s.len - n_all + (int)(last_row / a.R) + 1) : s.len;
-    const int least = a.causal ? s.len - n_all + (int)((int64_t)rt * kTileRows / a.R) + 1 : s.len;
-    const int full = s.len / kPage, units = (most + kPage - 1) / kPage, ufull = min(units, full);
-    const int32_t* table = a.kv.table + (int64_t)b * a.kv.max_pages;
+    const int heads = a.kv.seqs * a.kv.G, D = a.kv.D;
+    float2* const my_w = a.row_w + (size_t)blockIdx.x * a.kv.max_pages * kTileRows;
+    for (int64_t tile = blockIdx.x; tile < (int64_t)heads * row_tiles; tile += gridDim.x) {
+        // the longest tiles first; a head's tiles on one XCD (workgroup i runs on XCD i % 8), whose L2 its pages then are in
+        const int bg = (int)(tile % heads), rt = row_tiles - 1 - (int)(tile / heads);
+        const int b = bg / a.kv.G, g = bg % a.kv.G;
+        KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
+        const int n_all = s.n;
+        s.n = s.n < a.max_new ? s.n : a.max_new;
+        const int64_t rows = (int64_t)s.n * a.R;
+        if (rows <= kSplitRows || (int64_t)rt * kTileRows >= rows) continue;
+        const int64_t rr = (int64_t)rt * kTileRows + wid * 32 + c;
+        const bool live = rr < rows;
+        const int qi = (int)((live ? rr : rows - 1) / a.R), qh = g * a.R + (int)((live ? rr : rows - 1) % a.R);
+        const int lim = !live ? 0 : a.causal ? s.len - n_all + qi + 1 : s.len;
+        const int64_t last_row = min(rows, (int64_t)(rt + 1) * kTileRows) - 1;
+        const int most = a.causal ? max(0, s.len - n_all + (int)(last_row / a.R) + 1) : s.len;
+        const int least = last_row - (int64_t)rt * kTileRows + 1 < kTileRows ? 0 : a.causal ? s.len - n_all + (int)((int64_t)rt * kTileRows / a.R) + 1 : s.len;
+        const int full = s.len / kPage, units = (most + kPage - 1) / kPage, ufull = min(units, full);
+        const int32_t* table = a.kv.table + (int64_t)b * a.kv.max_pages;
 
-    bf16x8 q[NQ][KK];
+        bf16x8 q[NQ][KK];
 #pragma unroll
-    for (int k = 0; k < KK; ++k) {
-        bf16x8 p[NQ];
-        const int d = k * 16 + h * 8;
-        if (live && d < D) QParts<DT>::load(a, (s.first + qi) * a.q_token + qh * a.q_head + d, p);
+        for (int k = 0; k < KK; ++k) {
+            bf16x8 p[NQ];
+            const int d = k * 16 + h * 8;
+            if (live && d < D) QParts<DT>::load(a, (s.first + qi) * a.q_token + qh * a.q_head + d, p);
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) q[i][k] = live && d < D ? p[i] : bf16x8{};
-    }
-
-    // outputs are held in units of vref, the scale of some page; the same in all wavefronts
-    float m = -__builtin_inff(), l = 0.0f, vref = 0.0f, vmax = 0.0f;
-    f32x16 o[DL];
-#pragma unroll
-    for (int t = 0; t < DL; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
-
-    auto scores = [&](const uint16_t* keys, f32x16* sc) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sc[t][r] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < KK; ++k)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const bf16x8 w = *(const bf16x8*)(keys + ((t * KK + k) * 64 + lane) * 8);
-#pragma unroll
-                for (int i = 0; i < NQ; ++i) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[i][k], sc[t], 0, 0, 0);
-            }
-    };
-    auto softmax = [&](f32x16* sc, float factor, int u) {
-        const int base = u * kPage + h * 4;
-        float mx = -__builtin_inff();
-        if (u * kPage + kPage <= least) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) { sc[t][r] *= factor; mx = fmaxf(mx, sc[t][r]); }
-        } else {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    sc[t][r] = base + t * 32 + (r >> 2) * 8 + (r & 3) < lim ? sc[t][r] * factor : -__builtin_inff();
-                    mx = fmaxf(mx, sc[t][r]);
-                }
+            for (int i = 0; i < NQ; ++i) q[i][k] = live && d < D ? p[i] : bf16x8{};
         }
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float mn = fmaxf(m, mx), ms = mn == -__builtin_inff() ? 0.0f : mn;
-        const float alpha = exp2_of(m - ms), off = kPBias - ms;
-        float sum = 0.0f;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) { sc[t][r] = exp2_of(sc[t][r] + off); sum += sc[t][r]; }
-        if (__any(mn > m)) {
-#pragma unroll
-            for (int t = 0; t < DL; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[t][r] *= alpha;
-        }
-        m = mn;
-        l = __builtin_fmaf(l, alpha, sum);
-    };
-    auto rescale = [&](float f) {
+
+        // outputs are held in units of vref, the scale of some page; the same in all wavefronts
+        float m = -__builtin_inff(), l = 0.0f, vref = 0.0f, vmax = 0.0f;
+        f32x16 o[DL];
 #pragma unroll
         for (int t = 0; t < DL; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[t][r] *= f;
-    };
+            for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
 
-    uint4 kb[NR], vb[NR];
-    float ks = 0.0f, vs = 0.0f, ks_next = 0.0f, vs_next = 0.0f;
-    auto load = [&](int u) {
-        int64_t id = table[u];
-        const bool there = id >= 0 && id < a.kv.n_pages;
-        if (!there) id = 0;
-        const uint4* rec = (const uint4*)(a.kv.pages + kv_record(a.kv, id, g));
-        const float2 sc = *(const float2*)(a.kv.scales + (id * a.kv.G + g) * 2);
-        ks_next = there ? sc.x : __uint_as_float(0x7FC00000u);
-        vs_next = sc.y;
+        auto rescale = [&](float f) {
 #pragma unroll
-        for (int i = 0; i < NR; ++i)
-            if (i * 256 + tid < 4 * DP) {
-                kb[i] = rec[i * 256 + tid];
-                vb[i] = rec[4 * DP + i * 256 + tid];
-            }
-    };
-    auto stage = [&](uint16_t* to) {
+            for (int t = 0; t < DL; ++t)
 #pragma unroll
-        for (int i = 0; i < NR; ++i)
-            if (i * 256 + tid < 4 * DP) {
-                stage_keys<DP>(to, i * 256 + tid, kb[i]);
-                stage_values<DP>(to + PromptTile<DP>::kKeys, i * 256 + tid, vb[i]);
-            }
-    };
-    if (ufull > 0) {
-        load(0);
-        stage(x[0]);
-    }
-    for (int u = 0; u < ufull; ++u) {
-        ks = ks_next;
-        vs = vs_next;
-        __syncthreads();
-        if (u + 1 < ufull) load(u + 1);
-        const uint16_t *keys = x[u & 1], *values = keys + PromptTile<DP>::kKeys;
-        f32x16 sc[2];
-        scores(keys, sc);
-        softmax(sc, ks * a.scale, u);
-        // probabilities times vs / vref stay below 2^14 and keep their bits; a page of less than 2^-60 of the largest scale counts little enough
-        vmax = fmaxf(vmax, vs);
-        const float vt = fmaxf(vs, vmax * 0x1p-60f);
-        if (vs > 0.0f && (vt > 2.0f * vref || vt < vref * 0.015625f)) {
-            if (vref > 0.0f) rescale(vref / vt);
-            vref = vt;
-        }
-        const float ratio = vs > 0.0f ? vs / vref : 0.0f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            f16x8 p[NP];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float f = sc[k >> 1][(k & 1) * 8 + j] * ratio;
-                // the product is rounded to fp32 here: left alone, product and conversion become one instruction, whose result is in rare cases the other
-                // neighbour of the one that the rest is taken from, and a probability loses its second number
-                if constexpr (NP > 1) asm("" : "+v"(f));
-                const _Float16 hi = (_Float16)f;
-                p[0][j] = hi;
-                if constexpr (NP > 1) p[1][j] = (_Float16)(f - (float)hi);
-            }
-#pragma unroll
-            for (int t = 0; t < DL; ++t) {
-                const f16x8 v = *(const f16x8*)(values + ((t * 4 + k) * 64 + lane) * 8);
-#pragma unroll
-                for (int i = 0; i < NP; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[i], o[t], 0, 0, 0);
-            }
-        }
-        if (u + 1 < ufull) stage(x[(u + 1) & 1]);
-    }
-    if (units > full) {                                  // the tail
-        const int count = s.len - full * kPage;
-        __syncthreads();
-        stage_tail<DP>(x[0], x[0] + PromptTile<DP>::kKeys, a.kv.tails + kv_tail(a.kv, b, g), count, tid);
-        __syncthreads();
-        f32x16 sc[2];
-        scores(x[0], sc);
-        softmax(sc, a.scale, full);
-        rescale(vref);
-        const uint16_t* values = x[0] + PromptTile<DP>::kKeys;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            bf16x8 p[NB];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float f = sc[k >> 1][(k & 1) * 8 + j];
-#pragma unroll
-                for (int i = 0; i < NB; ++i) {
-                    p[i][j] = (__bf16)f;
-                    f -= (float)p[i][j];
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < DL; ++t) {
-                const bf16x8 v = *(const bf16x8*)(values + ((t * 4 + k) * 64 + lane) * 8);
-#pragma unroll
-                for (int i = 0; i < NB; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i], o[t], 0, 0, 0);
-            }
-        }
-    }
-    l += __shfl_xor(l, 32);
-    if (!live) return;
-    const float inv = l == 0.0f ? 0.0f : (units > full ? 1.0f : vref) / l;
-    const int64_t at = (s.first + qi) * a.H + qh;
-#pragma unroll
-    for (int t = 0; t < DL; ++t)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int d = t * 32 + k * 8 + h * 4;
-            if (d < D) store4<DT>(a.out, at * D + d, f32x4{o[t][k * 4], o[t][k * 4 + 1], o[t][k * 4 + 2], o[t][k * 4 + 3]} * inv);
-        }
-    if (h == 0) {
-        const float ms = m == -__builtin_inff() ? 0.0f : m;
-        if (a.lse) a.lse[at] = l == 0.0f ? -__builtin_inff() : (ms - kPBias + __log2f(l)) * kLn2;
-        if (a.mass) a.row_ml[at] = float2{ms, l == 0.0f ? 0.0f : 1.0f / l};
-    }
-}
-
-// Weights of the pages for the rows that are not split: a column's sum needs the rows' final sums, so scores are made once more (no second product, no
-// maximum).  A wavefront has a page, its keys in registers; four of them share the query rows, 32 at a time through LDS.  Every page has one
-// wavefront: nothing is added by atomics.
-template <int DT, int DP>
-__global__ __launch_bounds__(256, 1) void kv_mass_kernel(KvAttendArgs a, int page_tiles)
-{
-    constexpr int KK = DP / 16, NQ = QParts<DT>::N;
-    __shared__ __align__(16) uint16_t xq[NQ][KK * 64 * 8];
-    __shared__ float2 xml[32];
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 31, h = lane >> 5;
-    const int bg = blockIdx.x / page_tiles, b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
-    KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
-    const int n_all = s.n;
-    s.n = s.n < a.max_new ? s.n : a.max_new;
-    const int64_t rows = (int64_t)s.n * a.R;
-    const int pages = (s.len + kPage - 1) / kPage, full = s.len / kPage;
-    if (rows <= kSplitRows) return;
-    for (int p0 = blockIdx.x % page_tiles * 4; p0 < pages; p0 += page_tiles * 4) {
-        const int p = p0 + wid;
-        bf16x8 kf[2][KK];
-        float factor = a.scale;
-        if (p < full) {
-            int64_t id = a.kv.table[(int64_t)b * a.kv.max_pages + p];
-            const bool there = id >= 0 && id < a.kv.n_pages;
-            if (!there) id = 0;
-            const uint8_t* rec = a.kv.pages + kv_record(a.kv, id, g);
-            factor *= there ? a.kv.scales[(id * a.kv.G + g) * 2] : __uint_as_float(0x7FC00000u);
+                for (int r = 0; r < 16; ++r) o[t][r] *= f;
+        };
+        auto scores = [&](const uint16_t* keys, f32x16* sc) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int k = 0; k < KK; ++k) {
-                    // elements 16 k + 8 h + j of token 32 t + c: half c / 16 of the record of lane (2 (k % 2) + h) * 16 + c % 16
-                    const uint2 w = *(const uint2*)(rec + ((size_t)(t * (DP / 32) + (k >> 1)) * 64 + ((k & 1) * 2 + h) * 16 + (c & 15)) * 16 + (c >> 4) * 8);
-                    kf[t][k] = codes_bf16(w.x, w.y);
-                }
-        } else {
-            const uint16_t* tk = a.kv.tails + kv_tail(a.kv, b, g);
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int k = 0; k < KK; ++k) {
-                    uint4 w = {0, 0, 0, 0};
-                    if (p < pages && full * kPage + t * 32 + c < s.len) w = *(const uint4*)(tk + (t * 32 + c) * DP + k * 16 + h * 8);
-                    kf[t][k] = bf16_of(w);
-                }
-        }
-        // rows before the first that sees the first page of the workgroup add nothing
-        int64_t r0 = 0;
-        if (a.causal) {
-            const int64_t i0 = (int64_t)p0 * kPage - (s.len - n_all);       // query that sees it first
-            r0 = (i0 > 0 ? i0 * a.R : 0) & ~(int64_t)31;
-        }
-        float sum = 0.0f;
-        for (; r0 < rows; r0 += 32) {
-            __syncthreads();
-            for (int i = tid; i < KK * 64; i += 256) {
-                const int ll = i & 63, k = i >> 6, d = k * 16 + (ll >> 5) * 8;
-                const int64_t r = r0 + (ll & 31);
-                bf16x8 w[NQ];
-#pragma unroll
-                for (int j = 0; j < NQ; ++j) w[j] = bf16x8{};
-                if (r < rows && d < D) QParts<DT>::load(a, (s.first + r / a.R) * a.q_token + (g * a.R + r % a.R) * a.q_head + d, w);
-#pragma unroll
-                for (int j = 0; j < NQ; ++j) *(bf16x8*)&xq[j][i * 8] = w[j];
-            }
-            if (tid < 32) {
-                const int64_t r = r0 + tid;
-                xml[tid] = r < rows ? a.row_ml[(s.first + r / a.R) * a.H + g * a.R + r % a.R] : float2{0.0f, 0.0f};
-            }
-            __syncthreads();
-            const int64_t r = r0 + c;
-            const int lim = r >= rows ? 0 : a.causal ? s.len - n_all + (int)(r / a.R) + 1 : s.len;
-            const float2 ml = xml[c];
-            const float off = kPBias - ml.x;
-            f32x16 sc[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) sc[t][j] = 0.0f;
+                for (int r = 0; r < 16; ++r) sc[t][r] = 0.0f;
 #pragma unroll
             for (int k = 0; k < KK; ++k)
 #pragma unroll
-                for (int i = 0; i < NQ; ++i) {
-                    const bf16x8 w = *(const bf16x8*)&xq[i][(k * 64 + lane) * 8];
-                    sc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0][k], w, sc[0], 0, 0, 0);
-                    sc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[1][k], w, sc[1], 0, 0, 0);
-                }
-            float part = 0.0f;
+                for (int t = 0; t < 2; ++t) {
+                    const bf16x8 w = *(const bf16x8*)(keys + ((t * KK + k) * 64 + lane) * 8);
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float e = exp2_of(sc[t][j] * factor + off);
-                    part += p * kPage + t * 32 + (j >> 2) * 8 + h * 4 + (j & 3) < lim ? e : 0.0f;
+                    for (int i = 0; i < NQ; ++i) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[i][k], sc[t], 0, 0, 0);
                 }
-            // (a row that sees nothing of the page adds nothing, whatever its own sum is)
-            sum += part == 0.0f ? 0.0f : part * ml.y;
+        };
+        // scores -> probabilities times 2^8 and the page's scale over vref (lr: its logarithm, back: vref over it); the sum goes to l
+        auto softmax = [&](f32x16* sc, float factor, int u, float lr, float back) {
+            const int base = u * kPage + h * 4;
+            const bool all = u * kPage + kPage <= least;
+            float mx = -__builtin_inff();
+            if (all) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[t][r]);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, base + t * 32 + (r >> 2) * 8 + (r & 3) < lim ? sc[t][r] : -__builtin_inff());
+            }
+            float mine;
+            mx = other_half(mx, &mine);
+            mx = fmaxf(mx, mine) * factor;               // (the factor is not negative)
+            if (__any(mx > m + kSlack)) {
+                const float mn = fmaxf(m, mx), alpha = exp2_of(m - (mn == -__builtin_inff() ? 0.0f : mn));
+                rescale(alpha);
+                l *= alpha;
+                m = mn;
+            }
+            const float ms = m == -__builtin_inff() ? 0.0f : m, off = kPromptBias + lr - ms;
+            float sum = 0.0f;
+            if (all) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) { sc[t][r] = exp2_of(__builtin_fmaf(sc[t][r], factor, off)); sum += sc[t][r]; }
+            } else {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        sc[t][r] = base + t * 32 + (r >> 2) * 8 + (r & 3) < lim ? exp2_of(__builtin_fmaf(sc[t][r], factor, off)) : 0.0f;
+                        sum += sc[t][r];
+                    }
+            }
+            l = __builtin_fmaf(sum, back, l);
+            if (a.mass) {
+                sum = other_half(sum, &mine);
+                if (h == 0) my_w[(size_t)u * kTileRows + wid * 32 + c] = float2{ms, (sum + mine) * back};
+            }
+        };
+
+        uint4 kb[NR], vb[NR];
+        float ks = 0.0f, vs = 0.0f, ks_next = 0.0f, vs_next = 0.0f;
+        auto load = [&](int u) {
+            int64_t id = table[u];
+            const bool there = id >= 0 && id < a.kv.n_pages;
+            if (!there) id = 0;
+            const uint4* rec = (const uint4*)(a.kv.pages + kv_record(a.kv, id, g));
+            const float2 sc = *(const float2*)(a.kv.scales + (id * a.kv.G + g) * 2);
+            ks_next = there ? sc.x : __uint_as_float(0x7FC00000u);
+            vs_next = sc.y;
+#pragma unroll
+            for (int i = 0; i < NR; ++i)
+                if (i * 256 + tid < 4 * DP) {
+                    kb[i] = rec[i * 256 + tid];
+                    vb[i] = rec[4 * DP + i * 256 + tid];
+                }
+        };
+        auto stage = [&](uint16_t* to) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i)
+                if (i * 256 + tid < 4 * DP) {
+                    stage_keys<DP>(to, i * 256 + tid, kb[i]);
+                    stage_values<DP>(to + PromptTile<DP>::kKeys, i * 256 + tid, vb[i]);
+                }
+        };
+        __syncthreads();                                 // (the tile before may still be read)
+        if (ufull > 0) {
+            load(0);
+            stage(buf[0]);
         }
+        for (int u = 0; u < ufull; ++u) {
+            ks = ks_next;
+            vs = vs_next;
+            __syncthreads();
+            if (u + 1 < ufull) load(u + 1);
+            const uint16_t *keys = buf[u & 1], *values = keys + PromptTile<DP>::kKeys;
+            // the page's scale within 2^-6 .. 2 of vref, so that probabilities keep their bits; less than 2^-60 of the largest counts as that (a page
+            // of zeros: any)
+            vmax = fmaxf(vmax, vs);
+            const float vt = fmaxf(vs, vmax * 0x1p-60f);
+            if (vt > 2.0f * vref || (vs > 0.0f && vt < vref * 0.015625f)) {
+                if (vref > 0.0f) rescale(vref / vt);
+                vref = vt;
+            }
+            const float ratio = vs > 0.0f ? vt / vref : 1.0f;
+            f32x16 sc[2];
+            scores(keys, sc);
+            softmax(sc, ks * a.scale, u, __log2f(ratio), 1.0f / ratio);
 #pragma unroll
-        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0 && p < pages) {
-            float* to = a.mass + (int64_t)bg * a.kv.max_pages + p;
-            *to = a.decay == 0.0f ? sum : __builtin_fmaf(*to, a.decay, sum);
+            for (int k = 0; k < 4; ++k) {
+                f16x8 p[NP];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float f = sc[k >> 1][(k & 1) * 8 + j];
+                    const _Float16 hi = (_Float16)f;
+                    p[0][j] = hi;
+                    if constexpr (NP > 1) p[1][j] = (_Float16)(f - (float)hi);
+                }
+#pragma unroll
+                for (int t = 0; t < DL; ++t) {
+                    const f16x8 v = *(const f16x8*)(values + ((t * 4 + k) * 64 + lane) * 8);
+#pragma unroll
+                    for (int i = 0; i < NP; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[i], o[t], 0, 0, 0);
+                }
+            }
+            if (u + 1 < ufull) stage(buf[(u + 1) & 1]);
+        }
+        if (units > full) {                              // the tail
+            const int count = s.len - full * kPage;
+            __syncthreads();
+            stage_tail<DP>(buf[0], buf[0] + PromptTile<DP>::kKeys, a.kv.tails + kv_tail(a.kv, b, g), count, tid);
+            __syncthreads();
+            f32x16 sc[2];
+            scores(buf[0], sc);
+            rescale(vref);
+            vref = 1.0f;
+            softmax(sc, a.scale, full, 0.0f, 1.0f);
+            const uint16_t* values = buf[0] + PromptTile<DP>::kKeys;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                bf16x8 p[NB];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float f = sc[k >> 1][(k & 1) * 8 + j];
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) {
+                        p[i][j] = (__bf16)f;
+                        f -= (float)p[i][j];
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < DL; ++t) {
+                    const bf16x8 v = *(const bf16x8*)(values + ((t * 4 + k) * 64 + lane) * 8);
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[i], o[t], 0, 0, 0);
+                }
+            }
+        }
+        float mine;
+        l = other_half(l, &mine);
+        l += mine;
+        const float ms = m == -__builtin_inff() ? 0.0f : m;
+        if (live) {
+            const float inv = l == 0.0f ? 0.0f : vref / l;
+            const int64_t at = (s.first + qi) * a.H + qh;
+#pragma unroll
+            for (int t = 0; t < DL; ++t)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int d = t * 32 + k * 8 + h * 4;
+                    if (d < D) store4<DT>(a.out, at * D + d, f32x4{o[t][k * 4], o[t][k * 4 + 1], o[t][k * 4 + 2], o[t][k * 4 + 3]} * inv);
+                }
+            if (h == 0 && a.lse) a.lse[at] = l == 0.0f ? -__builtin_inff() : (ms - kPromptBias + __log2f(l)) * kLn2;
+        }
+        if (a.mass) {
+            // a page's sums of the tile's rows, now that the rows' own are known
+            if (h == 0) xrow[wid * 32 + c] = float2{ms, 1.0f / l};
+            __syncthreads();
+            const float2 r0 = xrow[lane], r1 = xrow[lane + 64];
+            float* to = a.tile_mass + ((int64_t)bg * row_tiles + rt) * a.kv.max_pages;
+            const int pages = (s.len + kPage - 1) / kPage;
+            for (int p0 = wid * 4; p0 < pages; p0 += 16) {       // four pages' loads at a time
+                float2 w[4][2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const size_t at = (size_t)min(p0 + e, max(units - 1, 0)) * kTileRows + lane;
+                    w[e][0] = my_w[at];
+                    w[e][1] = my_w[at + 64];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float sum = (w[e][0].y == 0.0f ? 0.0f : w[e][0].y * exp2_of(w[e][0].x - r0.x) * r0.y) + (w[e][1].y == 0.0f ? 0.0f : w[e][1].y * exp2_of(w[e][1].x - r1.x) * r1.y);
+#pragma unroll
+                    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+                    if (lane == 0 && p0 + e < pages) to[p0 + e] = p0 + e < units ? sum : 0.0f;
+                }
+            }
         }
     }
 }
+
+// The pages' weights over the row tiles, in their order.
+__device__ inline void kv_add_tiles(const KvAttendArgs& a, int row_tiles, int page_blocks)
+{
+    const int bg = blockIdx.x / page_blocks, b = bg / a.kv.G;
+    const KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
+    const int64_t rows = (int64_t)(s.n < a.max_new ? s.n : a.max_new) * a.R;
+    if (rows <= kSplitRows) return;
+    const int tiles = (int)((rows + kTileRows - 1) / kTileRows);
+    for (int p = blockIdx.x % page_blocks * 256 + threadIdx.x; p < (s.len + kPage - 1) / kPage; p += page_blocks * 256) {
+        const float* from = a.tile_mass + (int64_t)bg * row_tiles * a.kv.max_pages + p;
+        float sum = 0.0f;
+#pragma unroll 8
+        for (int t = 0; t < tiles; ++t) sum += from[(int64_t)t * a.kv.max_pages];
+        float* to = a.mass + (int64_t)bg * a.kv.max_pages + p;
+        *to = a.decay == 0.0f ? sum : __builtin_fmaf(*to, a.decay, sum);
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void kv_mass_kernel(KvAttendArgs a, int row_tiles, int page_blocks) { kv_add_tiles(a, row_tiles, page_blocks); }
 
 }  // namespace slicer

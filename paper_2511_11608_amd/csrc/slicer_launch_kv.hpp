@@ -23,7 +23,8 @@ struct KvAttendLaunch {
     int split_tiles;          // their tiles
     int row_blocks, page_blocks;
     int prompt_tiles;         // row tiles of 128; 0: no sequence can have that many rows
-    int mass_tiles;           // four pages each
+    int prompt_slots;         // workgroups that keep weights on the way
+    int mass_blocks;          // 256 pages each; 0: no weights
 };
 
 template <int DT> hipError_t launch_kv_append(const KvAppendArgs& a, int64_t blocks, hipStream_t st);
@@ -79,9 +80,9 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, const KvAttendLaunch& p, hipS
                 hipLaunchKernelGGL((kv_join_kernel<DT, DP>), dim3(pairs * (unsigned)(p.row_blocks + p.page_blocks)), dim3(256), 0, st, a, p.row_blocks, p.page_blocks, p.tile_rows);
         }
         if (p.prompt_tiles) {
-            hipLaunchKernelGGL((kv_prompt_kernel<DT, DP>), dim3(pairs * (unsigned)p.prompt_tiles), dim3(256), 0, st, a, p.prompt_tiles);
-            if (p.mass_tiles)
-                hipLaunchKernelGGL((kv_mass_kernel<DT, DP>), dim3(pairs * (unsigned)p.mass_tiles), dim3(256), 0, st, a, p.mass_tiles);
+            const unsigned tiles = pairs * (unsigned)p.prompt_tiles;
+            hipLaunchKernelGGL((kv_prompt_kernel<DT, DP>), dim3(p.mass_blocks ? std::min(tiles, (unsigned)p.prompt_slots) : tiles), dim3(256), 0, st, a, p.prompt_tiles);
+            if (p.mass_blocks) hipLaunchKernelGGL((kv_mass_kernel<DT>), dim3(pairs * (unsigned)p.mass_blocks), dim3(256), 0, st, a, p.prompt_tiles, p.mass_blocks);
         }
     });
     return hipGetLastError();

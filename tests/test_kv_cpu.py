@@ -54,7 +54,7 @@ def test_shapes_that_are_refused(lib):
         assert lib.slicer_kv_sizes(C.byref(kv), None, None, None) == -1, kw
         for call in (append, attend, read, evict):
             assert call(lib, kv) == -1, (kw, call)
-        assert lib.slicer_kv_attend_sizes(C.byref(kv), 8, 2, 1, 100, None) == -1
+        assert lib.slicer_kv_attend_sizes(C.byref(kv), 8, 2, 1, 100, 1, None) == -1
     assert lib.slicer_kv_sizes(None, None, None, None) == -1
     for call in (append, attend, read, evict):
         assert call(lib, None) == -1
@@ -83,8 +83,8 @@ def test_null_pointers_types_and_counts_are_refused(lib):
         assert evict(lib, kv, outs=tuple(None if j == i else 256 for j in range(5))) == -1
     assert evict(lib, kv, keep=-1, sink=0, recent=0) == -1 and evict(lib, kv, sink=-1) == -1 and evict(lib, kv, recent=-1) == -1
     assert evict(lib, kv, keep=2, sink=2, recent=1) == -1 and evict(lib, kv, keep=2 ** 31 - 1, sink=2 ** 31 - 1, recent=2 ** 31 - 1) == -1
-    assert lib.slicer_kv_attend_sizes(C.byref(kv), 6, 2, 1, 100, None) == -1 and lib.slicer_kv_attend_sizes(C.byref(kv), 8, 2, 0, 100, None) == -1
-    assert lib.slicer_kv_attend_sizes(C.byref(kv), 8, 2, 1, -1, None) == -1
+    assert lib.slicer_kv_attend_sizes(C.byref(kv), 6, 2, 1, 100, 1, None) == -1 and lib.slicer_kv_attend_sizes(C.byref(kv), 8, 2, 0, 100, 1, None) == -1
+    assert lib.slicer_kv_attend_sizes(C.byref(kv), 8, 2, 1, -1, 1, None) == -1
 
 
 def test_workspace_covers_every_split(lib):
@@ -93,12 +93,15 @@ def test_workspace_covers_every_split(lib):
     for seqs, G, D, P, H, tokens, max_new, max_len in ((1, 8, 128, 4096, 32, 1, 1, 262144), (256, 8, 128, 32, 64, 256, 1, 2048), (3, 2, 80, 40, 10, 900, 400, 2000),
                                                        (1, 1, 8, 1, 1, 1, 1, 0)):
         kv = handle(seqs=seqs, kv_heads=G, head_dim=D, max_pages=P)
-        assert lib.slicer_kv_attend_sizes(C.byref(kv), H, tokens, max_new, max_len, C.byref(w)) == 0
-        rows = min(64, min(tokens, max_new) * (H // G))
-        assert w.value >= seqs * G * rows * 8 * (P + 1)
-        assert w.value >= (tokens * H * 8 if max_new * (H // G) > 64 else 0)
-        assert w.value < 1 << 30
-    assert lib.slicer_kv_attend_sizes(C.byref(kv), 1, 0, 0, 0, C.byref(w)) == 0 and w.value == 0
+        assert lib.slicer_kv_attend_sizes(C.byref(kv), H, tokens, max_new, max_len, 1, C.byref(w)) == 0
+        rows, with_mass = min(64, min(tokens, max_new) * (H // G)), w.value
+        assert with_mass >= seqs * G * rows * 8 * (P + 1)
+        tiles = -(-max_new * (H // G) // 128) if max_new * (H // G) > 64 else 0
+        assert with_mass >= min(seqs * G * tiles, 256) * P * 1024 + seqs * G * tiles * P * 4
+        assert with_mass < 1 << 31
+        assert lib.slicer_kv_attend_sizes(C.byref(kv), H, tokens, max_new, max_len, 0, C.byref(w)) == 0
+        assert seqs * G * rows * 8 <= w.value < with_mass
+    assert lib.slicer_kv_attend_sizes(C.byref(kv), 1, 0, 0, 0, 1, C.byref(w)) == 0 and w.value == 0
 
 
 def test_the_binding_refuses_what_is_not_on_the_gpu(lib):
