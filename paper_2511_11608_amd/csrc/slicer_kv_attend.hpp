@@ -176,9 +176,9 @@ __global__ __launch_bounds__(256, (QT == 1 && DP <= 160) || (QT == 1 && DP == 19
 
     // scores of a page -> probabilities (times 2^13), the running maximum and sum; returns what the sums so far are to be multiplied by
     auto softmax = [&](int x, f32x4* sc, float factor, int u) {
-        const int base = u * kPage;
+        const int left = lim[x] - u * kPage - gq * 4;    // tokens that the row sees from the lane's first on
         float mx = -__builtin_inff();
-        if (base + kPage <= least) {
+        if (u * kPage + kPage <= least) {
 #pragma unroll
             for (int T = 0; T < 4; ++T)
 #pragma unroll
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, (QT == 1 && DP <= 160) || (QT == 1 && DP == 19
             for (int T = 0; T < 4; ++T)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    sc[T][r] = base + T * 16 + gq * 4 + r < lim[x] ? sc[T][r] * factor : -__builtin_inff();
+                    sc[T][r] = T * 16 + r < left ? sc[T][r] * factor : -__builtin_inff();
                     mx = fmaxf(mx, sc[T][r]);
                 }
         }
@@ -588,6 +588,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
 {
     constexpr int KK = DP / 16, DL = DP / 32, NQ = QParts<DT>::N, NP = QParts<DT>::NP, NB = QParts<DT>::NB;
     constexpr int NR = (4 * DP + 255) / 256;             // records of keys (and of values) a thread
+    constexpr int kAhead = KK < 4 ? 2 : 6;
     __shared__ __align__(16) uint16_t buf[2][PromptTile<DP>::kAll];
     __shared__ float2 xrow[kTileRows];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 31, h = lane >> 5;
@@ -613,13 +614,14 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         const int32_t* table = a.kv.table + (int64_t)b * a.kv.max_pages;
 
         bf16x8 q[NQ][KK];
+        const int64_t q_at = (s.first + qi) * a.q_token + qh * a.q_head + h * 8;
 #pragma unroll
         for (int k = 0; k < KK; ++k) {
             bf16x8 p[NQ];
-            const int d = k * 16 + h * 8;
-            if (live && d < D) QParts<DT>::load(a, (s.first + qi) * a.q_token + qh * a.q_head + d, p);
+            const bool there = live && k * 16 < D - h * 8;
+            if (there) QParts<DT>::load(a, q_at + k * 16, p);
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) q[i][k] = live && d < D ? p[i] : bf16x8{};
+            for (int i = 0; i < NQ; ++i) q[i][k] = there ? p[i] : bf16x8{};
         }
 
         // outputs are held in units of vref, the scale of some page; the same in all wavefronts
@@ -649,10 +651,18 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
 #pragma unroll
                     for (int i = 0; i < NQ; ++i) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[i][k], sc[t], 0, 0, 0);
                 }
+            // operands are asked for kAhead products before they are used
+            __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+            for (int i = 0; i < 2 * KK - kAhead; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, NQ, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, NQ * kAhead, 0);
         };
         // scores -> probabilities times 2^8 and the page's scale over vref (lr: its logarithm, back: vref over it); the sum goes to l
         auto softmax = [&](f32x16* sc, float factor, int u, float lr, float back) {
-            const int base = u * kPage + h * 4;
+            const int left = lim - u * kPage - h * 4;    // tokens that the row sees from the lane's first on
             const bool all = u * kPage + kPage <= least;
             float mx = -__builtin_inff();
             if (all) {
@@ -664,7 +674,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, base + t * 32 + (r >> 2) * 8 + (r & 3) < lim ? sc[t][r] : -__builtin_inff());
+                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, t * 32 + (r >> 2) * 8 + (r & 3) < left ? sc[t][r] : -__builtin_inff());
             }
             float mine;
             mx = other_half(mx, &mine);
@@ -687,7 +697,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        sc[t][r] = base + t * 32 + (r >> 2) * 8 + (r & 3) < lim ? exp2_of(__builtin_fmaf(sc[t][r], factor, off)) : 0.0f;
+                        sc[t][r] = t * 32 + (r >> 2) * 8 + (r & 3) < left ? exp2_of(__builtin_fmaf(sc[t][r], factor, off)) : 0.0f;
                         sum += sc[t][r];
                     }
             }
@@ -699,15 +709,23 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         };
 
         uint4 kb[NR], vb[NR];
-        float ks = 0.0f, vs = 0.0f, ks_next = 0.0f, vs_next = 0.0f;
+        // places and scales of 64 pages lie in the lanes
+        u32 my_page = 0;
+        float my_ks = 0.0f, my_vs = 0.0f;
+        auto fetch = [&](int u) {
+            my_page = 0;
+            my_ks = my_vs = 0.0f;
+            if (u + lane < ufull) {
+                const int64_t id = table[u + lane];
+                const bool there = id >= 0 && id < a.kv.n_pages;
+                my_page = there ? (u32)id : 0u;
+                const float2 sc = *(const float2*)(a.kv.scales + ((int64_t)my_page * a.kv.G + g) * 2);
+                my_ks = there ? sc.x : __uint_as_float(0x7FC00000u);
+                my_vs = sc.y;
+            }
+        };
         auto load = [&](int u) {
-            int64_t id = table[u];
-            const bool there = id >= 0 && id < a.kv.n_pages;
-            if (!there) id = 0;
-            const uint4* rec = (const uint4*)(a.kv.pages + kv_record(a.kv, id, g));
-            const float2 sc = *(const float2*)(a.kv.scales + (id * a.kv.G + g) * 2);
-            ks_next = there ? sc.x : __uint_as_float(0x7FC00000u);
-            vs_next = sc.y;
+            const uint4* rec = (const uint4*)(a.kv.pages + kv_record(a.kv, bcast(my_page, u & 63), g));
 #pragma unroll
             for (int i = 0; i < NR; ++i)
                 if (i * 256 + tid < 4 * DP) {
@@ -725,14 +743,17 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         };
         __syncthreads();                                 // (the tile before may still be read)
         if (ufull > 0) {
+            fetch(0);
             load(0);
             stage(buf[0]);
         }
         for (int u = 0; u < ufull; ++u) {
-            ks = ks_next;
-            vs = vs_next;
+            const float ks = __uint_as_float(bcast(__float_as_uint(my_ks), u & 63)), vs = __uint_as_float(bcast(__float_as_uint(my_vs), u & 63));
             __syncthreads();
-            if (u + 1 < ufull) load(u + 1);
+            if (u + 1 < ufull) {
+                if (((u + 1) & 63) == 0) fetch(u + 1);
+                load(u + 1);
+            }
             const uint16_t *keys = buf[u & 1], *values = keys + PromptTile<DP>::kKeys;
             // the page's scale within 2^-6 .. 2 of vref, so that probabilities keep their bits; less than 2^-60 of the largest counts as that (a page
             // of zeros: any)
@@ -745,9 +766,16 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
             const float ratio = vs > 0.0f ? vt / vref : 1.0f;
             f32x16 sc[2];
             scores(keys, sc);
-            softmax(sc, ks * a.scale, u, __log2f(ratio), 1.0f / ratio);
+            f16x8 v[2][DL];
+#pragma unroll
+            for (int t = 0; t < DL; ++t) v[0][t] = *(const f16x8*)(values + (t * 4 * 64 + lane) * 8);
+            softmax(sc, ks * a.scale, u, __log2f(ratio), __builtin_amdgcn_rcpf(ratio));
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
+                if (k < 3) {
+#pragma unroll
+                    for (int t = 0; t < DL; ++t) v[(k + 1) & 1][t] = *(const f16x8*)(values + ((t * 4 + k + 1) * 64 + lane) * 8);
+                }
                 f16x8 p[NP];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -757,11 +785,9 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                     if constexpr (NP > 1) p[1][j] = (_Float16)(f - (float)hi);
                 }
 #pragma unroll
-                for (int t = 0; t < DL; ++t) {
-                    const f16x8 v = *(const f16x8*)(values + ((t * 4 + k) * 64 + lane) * 8);
+                for (int t = 0; t < DL; ++t)
 #pragma unroll
-                    for (int i = 0; i < NP; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[i], o[t], 0, 0, 0);
-                }
+                    for (int i = 0; i < NP; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[k & 1][t], p[i], o[t], 0, 0, 0);
             }
             if (u + 1 < ufull) stage(buf[(u + 1) & 1]);
         }
@@ -802,13 +828,13 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         const float ms = m == -__builtin_inff() ? 0.0f : m;
         if (live) {
             const float inv = l == 0.0f ? 0.0f : vref / l;
-            const int64_t at = (s.first + qi) * a.H + qh;
+            const int64_t at = (s.first + qi) * a.H + qh, out_at = at * D + h * 4;
 #pragma unroll
             for (int t = 0; t < DL; ++t)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int d = t * 32 + k * 8 + h * 4;
-                    if (d < D) store4<DT>(a.out, at * D + d, f32x4{o[t][k * 4], o[t][k * 4 + 1], o[t][k * 4 + 2], o[t][k * 4 + 3]} * inv);
+                    const int d = t * 32 + k * 8;
+                    if (d < D - h * 4) store4<DT>(a.out, out_at + d, f32x4{o[t][k * 4], o[t][k * 4 + 1], o[t][k * 4 + 2], o[t][k * 4 + 3]} * inv);
                 }
             if (h == 0 && a.lse) a.lse[at] = l == 0.0f ? -__builtin_inff() : (ms - kPromptBias + __log2f(l)) * kLn2;
         }
