@@ -609,7 +609,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         const int lim = !live ? 0 : a.causal ? s.len - n_all + qi + 1 : s.len;
         const int64_t last_row = min(rows, (int64_t)(rt + 1) * kTileRows) - 1;
         const int most = a.causal ? max(0, s.len - n_all + (int)(last_row / a.R) + 1) : s.len;
-        const int least = last_row - (int64_t)rt * kTileRows + 1 < kTileRows ? 0 : a.causal ? s.len - n_all + (int)((int64_t)rt * kTileRows / a.R) + 1 : s.len;
+        const int least = a.causal ? s.len - n_all + (int)((int64_t)rt * kTileRows / a.R) + 1 : s.len;
         const int full = s.len / kPage, units = (most + kPage - 1) / kPage, ufull = min(units, full);
         const int32_t* table = a.kv.table + (int64_t)b * a.kv.max_pages;
 
@@ -651,64 +651,9 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
 #pragma unroll
                     for (int i = 0; i < NQ; ++i) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[i][k], sc[t], 0, 0, 0);
                 }
-            // operands are asked for kAhead products before they are used
-            __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
-#pragma unroll
-            for (int i = 0; i < 2 * KK - kAhead; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, NQ, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, NQ * kAhead, 0);
         };
-        // scores -> probabilities times 2^8 and the page's scale over vref (lr: its logarithm, back: vref over it); the sum goes to l
-        auto softmax = [&](f32x16* sc, float factor, int u, float lr, float back) {
-            const int left = lim - u * kPage - h * 4;    // tokens that the row sees from the lane's first on
-            const bool all = u * kPage + kPage <= least;
-            float mx = -__builtin_inff();
-            if (all) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[t][r]);
-            } else {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, t * 32 + (r >> 2) * 8 + (r & 3) < left ? sc[t][r] : -__builtin_inff());
-            }
-            float mine;
-            mx = other_half(mx, &mine);
-            mx = fmaxf(mx, mine) * factor;               // (the factor is not negative)
-            if (__any(mx > m + kSlack)) {
-                const float mn = fmaxf(m, mx), alpha = exp2_of(m - (mn == -__builtin_inff() ? 0.0f : mn));
-                rescale(alpha);
-                l *= alpha;
-                m = mn;
-            }
-            const float ms = m == -__builtin_inff() ? 0.0f : m, off = kPromptBias + lr - ms;
-            float sum = 0.0f;
-            if (all) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) { sc[t][r] = exp2_of(__builtin_fmaf(sc[t][r], factor, off)); sum += sc[t][r]; }
-            } else {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        sc[t][r] = t * 32 + (r >> 2) * 8 + (r & 3) < left ? exp2_of(__builtin_fmaf(sc[t][r], factor, off)) : 0.0f;
-                        sum += sc[t][r];
-                    }
-            }
-            l = __builtin_fmaf(sum, back, l);
-            if (a.mass) {
-                sum = other_half(sum, &mine);
-                if (h == 0) my_w[(size_t)u * kTileRows + wid * 32 + c] = float2{ms, (sum + mine) * back};
-            }
-        };
-
         uint4 kb[NR], vb[NR];
+        auto mine = [&](int i) { return DP % 64 == 0 || i * 256 + tid < 4 * DP; };      // whether the thread's i-th record is one
         // places and scales of 64 pages lie in the lanes
         u32 my_page = 0;
         float my_ks = 0.0f, my_vs = 0.0f;
@@ -724,52 +669,88 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                 my_vs = sc.y;
             }
         };
-        auto load = [&](int u) {
-            const uint4* rec = (const uint4*)(a.kv.pages + kv_record(a.kv, bcast(my_page, u & 63), g));
+        auto load_keys = [&](int lane_of) {
+            const uint4* rec = (const uint4*)(a.kv.pages + kv_record(a.kv, bcast(my_page, lane_of), g));
 #pragma unroll
             for (int i = 0; i < NR; ++i)
-                if (i * 256 + tid < 4 * DP) {
-                    kb[i] = rec[i * 256 + tid];
-                    vb[i] = rec[4 * DP + i * 256 + tid];
-                }
+                if (mine(i)) kb[i] = rec[i * 256 + tid];
         };
-        auto stage = [&](uint16_t* to) {
+        auto load_values = [&](int lane_of) {
+            const uint4* rec = (const uint4*)(a.kv.pages + kv_record(a.kv, bcast(my_page, lane_of), g)) + 4 * DP;
 #pragma unroll
             for (int i = 0; i < NR; ++i)
-                if (i * 256 + tid < 4 * DP) {
-                    stage_keys<DP>(to, i * 256 + tid, kb[i]);
-                    stage_values<DP>(to + PromptTile<DP>::kKeys, i * 256 + tid, vb[i]);
-                }
+                if (mine(i)) vb[i] = rec[i * 256 + tid];
         };
-        __syncthreads();                                 // (the tile before may still be read)
-        if (ufull > 0) {
-            fetch(0);
-            load(0);
-            stage(buf[0]);
-        }
-        for (int u = 0; u < ufull; ++u) {
-            const float ks = __uint_as_float(bcast(__float_as_uint(my_ks), u & 63)), vs = __uint_as_float(bcast(__float_as_uint(my_vs), u & 63));
-            __syncthreads();
-            if (u + 1 < ufull) {
-                if (((u + 1) & 63) == 0) fetch(u + 1);
-                load(u + 1);
-            }
-            const uint16_t *keys = buf[u & 1], *values = keys + PromptTile<DP>::kKeys;
-            // the page's scale within 2^-6 .. 2 of vref, so that probabilities keep their bits; less than 2^-60 of the largest counts as that (a page
-            // of zeros: any)
+        auto stage_k = [&](int which) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i)
+                if (mine(i)) stage_keys<DP>(buf[which], i * 256 + tid, kb[i]);
+        };
+        auto stage_v = [&](int which) {
+#pragma unroll
+            for (int i = 0; i < NR; ++i)
+                if (mine(i)) stage_values<DP>(buf[which] + PromptTile<DP>::kKeys, i * 256 + tid, vb[i]);
+        };
+        // what page u's scores are multiplied by, and its value scale over vref with its logarithm and inverse; vref follows the scales: within
+        // 2^-6 .. 2 of a page's, so that probabilities keep their bits; less than 2^-60 of the largest counts as that (a page of zeros: any)
+        float factor = 0.0f, lr = 0.0f, back = 1.0f;
+        auto page_scales = [&](int lane_of) {
+            const float ks = __uint_as_float(bcast(__float_as_uint(my_ks), lane_of)), vs = __uint_as_float(bcast(__float_as_uint(my_vs), lane_of));
+            factor = ks * a.scale;
             vmax = fmaxf(vmax, vs);
             const float vt = fmaxf(vs, vmax * 0x1p-60f);
             if (vt > 2.0f * vref || (vs > 0.0f && vt < vref * 0.015625f)) {
                 if (vref > 0.0f) rescale(vref / vt);
                 vref = vt;
             }
-            const float ratio = vs > 0.0f ? vt / vref : 1.0f;
-            f32x16 sc[2];
-            scores(keys, sc);
+            const float ratio = vs > 0.0f ? vt * __builtin_amdgcn_rcpf(vref) : 1.0f;
+            lr = __log2f(ratio);
+            back = __builtin_amdgcn_rcpf(ratio);
+        };
+        // a new maximum of the lane's scores: the sums so far are scaled down to it where it is far above the old one
+        auto new_maximum = [&](float mx) {
+            float here;
+            mx = other_half(mx, &here);
+            mx = fmaxf(mx, here) * factor;               // (the factor is not negative)
+            if (__any(mx > m + kSlack)) {
+                const float mn = fmaxf(m, mx), alpha = exp2_of(m - (mn == -__builtin_inff() ? 0.0f : mn));
+                rescale(alpha);
+                l *= alpha;
+                m = mn;
+            }
+        };
+        auto page_weight = [&](int u, float sum) {
+            if (a.mass) {
+                float here;
+                sum = other_half(sum, &here);
+                if (h == 0) my_w[(size_t)u * kTileRows + wid * 32 + c] = float2{m == -__builtin_inff() ? 0.0f : m, (sum + here) * back};
+            }
+        };
+        // scores -> probabilities times 2^8 and the page's scale over vref; the sum goes to l
+        auto softmax = [&](f32x16* sc, int u) {
+            const int left = lim - u * kPage - h * 4;    // tokens that the row sees from the lane's first on
+            float mx = -__builtin_inff();
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, t * 32 + (r >> 2) * 8 + (r & 3) < left ? sc[t][r] : -__builtin_inff());
+            new_maximum(mx);
+            const float off = kPromptBias + lr - (m == -__builtin_inff() ? 0.0f : m);
+            float sum = 0.0f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    sc[t][r] = t * 32 + (r >> 2) * 8 + (r & 3) < left ? exp2_of(__builtin_fmaf(sc[t][r], factor, off)) : 0.0f;
+                    sum += sc[t][r];
+                }
+            l = __builtin_fmaf(sum, back, l);
+            page_weight(u, sum);
+        };
+        auto products = [&](const uint16_t* values, const f32x16* sc) {
             f16x8 v[2][DL];
 #pragma unroll
             for (int t = 0; t < DL; ++t) v[0][t] = *(const f16x8*)(values + (t * 4 * 64 + lane) * 8);
-            softmax(sc, ks * a.scale, u, __log2f(ratio), __builtin_amdgcn_rcpf(ratio));
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (k < 3) {
@@ -789,7 +770,162 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
 #pragma unroll
                     for (int i = 0; i < NP; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[k & 1][t], p[i], o[t], 0, 0, 0);
             }
-            if (u + 1 < ufull) stage(buf[(u + 1) & 1]);
+        };
+
+        __syncthreads();                                 // (the tile before may still be read)
+        // Pages that every row sees whole, in a pipeline: while a page's probabilities are made and multiplied by its values, the next page's scores are
+        // made, and the operands of the keys behind those and of the next values go to LDS: matrix and vector instructions of one wavefront
+        // run at the same time.  Page u has its keys in buf[u % 2] one step before its values.
+        const int whole = min(ufull, max(least, 0) / kPage);
+        int u0 = 0;
+        if (whole >= 2) {
+            int base = 0;                                // page of the lanes' first place
+            fetch(0);
+            load_keys(0);
+            load_values(0);
+            stage_k(0);
+            stage_v(0);
+            load_keys(1);
+            stage_k(1);
+            __syncthreads();
+            load_keys(min(2, whole - 1));
+            load_values(1);
+            f32x16 sa[2], sb[2];
+            scores(buf[0], sa);
+            __syncthreads();                             // (the first step writes the keys of page 2 there)
+            page_scales(0);
+            {
+                float mx = -__builtin_inff();
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sa[t][r]);
+                new_maximum(mx);
+            }
+            auto exponentials = [&](f32x16* sc) {
+                const float off = kPromptBias + lr - (m == -__builtin_inff() ? 0.0f : m);
+                float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) { sc[t][r] = exp2_of(__builtin_fmaf(sc[t][r], factor, off)); part[r & 3] += sc[t][r]; }
+                const float sum = (part[0] + part[1]) + (part[2] + part[3]);
+                l = __builtin_fmaf(sum, back, l);
+                return sum;
+            };
+            auto step = [&](int u, f32x16* sc, f32x16* next) {
+#if VAR == 3
+                __builtin_amdgcn_s_setprio(1);
+#endif
+                scores(buf[(u + 1) & 1], next);
+#if VAR == 3
+                __builtin_amdgcn_s_setprio(0);
+#endif
+                const float sum = exponentials(sc);
+#if VAR == 3
+                __builtin_amdgcn_s_setprio(1);
+#endif
+                products(buf[u & 1] + PromptTile<DP>::kKeys, sc);
+#if VAR == 3
+                __builtin_amdgcn_s_setprio(0);
+#endif
+                stage_k(u & 1);
+                stage_v((u + 1) & 1);
+                float mx = -__builtin_inff();
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, next[t][r]);
+                // the order of all this: operands from LDS kAhead products before they are used, the exponentials between the next page's products,
+                // conversions and what goes to LDS between this page's
+#if VAR == 2
+                __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+                for (int i = 0; i < 2 * KK; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, NQ, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 64 / KK / 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x400, 32 / KK / 2, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4 * DL; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);
+                    if (i < 4 * DL - kAhead) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+                }
+#elif VAR == 4
+#pragma unroll
+                for (int i = 0; i < 2 * KK; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, NQ, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x400, 32 / KK / 2, 0);
+                }
+#elif VAR == 5
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+                for (int i = 0; i < 2 * KK; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, NQ, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x400, 32 / KK / 2, 0);
+                }
+#elif VAR == 6
+                __builtin_amdgcn_iglp_opt(0);
+#elif VAR == 7
+                __builtin_amdgcn_iglp_opt(1);
+#endif
+                page_weight(u, sum);
+                if (u + 4 - base > 64) {                 // (places up to u + 3 are asked for below)
+                    base = u;
+                    fetch(u);
+                }
+                load_keys(min(u + 3, whole - 1) - base);
+                load_values(min(u + 2, whole - 1) - base);
+                page_scales(u + 1 - base);
+                new_maximum(mx);
+                __syncthreads();
+            };
+            int u = 0;
+            for (; u + 2 < whole; u += 2) {
+                step(u, sa, sb);
+                step(u + 1, sb, sa);
+            }
+            if (u + 1 < whole) {
+                step(u, sa, sb);
+                ++u;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) sa[t] = sb[t];
+            }
+            const float sum = exponentials(sa);
+            products(buf[u & 1] + PromptTile<DP>::kKeys, sa);
+            page_weight(u, sum);
+            u0 = whole;
+            __syncthreads();
+        }
+        // the others, one at a time
+        if (u0 < ufull) {
+            fetch(u0);
+            load_keys(0);
+            load_values(0);
+            stage_k(0);
+            stage_v(0);
+        }
+        for (int u = u0; u < ufull; ++u) {
+            const int at = (u - u0) & 63;
+            page_scales(at);
+            __syncthreads();
+            if (u + 1 < ufull) {
+                if (at == 63) fetch(u + 1);
+                load_keys((at + 1) & 63);
+                load_values((at + 1) & 63);
+            }
+            const int which = (u - u0) & 1;
+            f32x16 sc[2];
+            scores(buf[which], sc);
+            softmax(sc, u);
+            products(buf[which] + PromptTile<DP>::kKeys, sc);
+            if (u + 1 < ufull) {
+                stage_k(which ^ 1);
+                stage_v(which ^ 1);
+            }
         }
         if (units > full) {                              // the tail
             const int count = s.len - full * kPage;
@@ -800,7 +936,10 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
             scores(buf[0], sc);
             rescale(vref);
             vref = 1.0f;
-            softmax(sc, a.scale, full, 0.0f, 1.0f);
+            factor = a.scale;
+            lr = 0.0f;
+            back = 1.0f;
+            softmax(sc, full);
             const uint16_t* values = buf[0] + PromptTile<DP>::kKeys;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -822,9 +961,9 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                 }
             }
         }
-        float mine;
-        l = other_half(l, &mine);
-        l += mine;
+        float here;
+        l = other_half(l, &here);
+        l += here;
         const float ms = m == -__builtin_inff() ? 0.0f : m;
         if (live) {
             const float inv = l == 0.0f ? 0.0f : vref / l;
@@ -840,7 +979,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         }
         if (a.mass) {
             // a page's sums of the tile's rows, now that the rows' own are known
-            if (h == 0) xrow[wid * 32 + c] = float2{ms, 1.0f / l};
+            if (h == 0) xrow[wid * 32 + c] = float2{ms, live ? 1.0f / l : 0.0f};
             __syncthreads();
             const float2 r0 = xrow[lane], r1 = xrow[lane + 64];
             float* to = a.tile_mass + ((int64_t)bg * row_tiles + rt) * a.kv.max_pages;
@@ -855,7 +994,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float sum = (w[e][0].y == 0.0f ? 0.0f : w[e][0].y * exp2_of(w[e][0].x - r0.x) * r0.y) + (w[e][1].y == 0.0f ? 0.0f : w[e][1].y * exp2_of(w[e][1].x - r1.x) * r1.y);
+                    float sum = (w[e][0].y == 0.0f || r0.y == 0.0f ? 0.0f : w[e][0].y * exp2_of(w[e][0].x - r0.x) * r0.y) + (w[e][1].y == 0.0f || r1.y == 0.0f ? 0.0f : w[e][1].y * exp2_of(w[e][1].x - r1.x) * r1.y);
 #pragma unroll
                     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
                     if (lane == 0 && p0 + e < pages) to[p0 + e] = p0 + e < units ? sum : 0.0f;
