@@ -63,9 +63,9 @@ int64_t blocks_of(int64_t tokens, int max_new) { return (std::min<int64_t>(token
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 struct AttendPlan {
-    int splits, rows_pad;
+    int splits, rows_pad, few_rows, prompt_splits, slot_pages;
     KvAttendLaunch launch;
-    size_t off_part_ml, off_part_o, off_page_w, off_row_w, off_tile_mass, total;
+    size_t off_part_ml, off_part_o, off_page_w, off_prompt_ml, off_prompt_o, off_row_total, off_row_w, off_tile_mass, total;
 };
 
 AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_new, int64_t max_len, bool mass)
@@ -74,26 +74,40 @@ AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_n
     const int64_t pairs = (int64_t)kv->seqs * kv->kv_heads, R = heads / kv->kv_heads;
     const int64_t rows = std::min<int64_t>(std::min<int64_t>(tokens, max_new) * R, (int64_t)1 << 31);
     const int64_t pages = std::min<int64_t>(kv->max_pages, (std::max<int64_t>(max_len, 1) + kPage - 1) / kPage);
-    p.rows_pad = (int)std::min<int64_t>(rows, kSplitRows);
-    p.launch.tile_rows = p.rows_pad > 16 && round32(kv->head_dim) <= kWideTile ? 32 : 16;
+    const int64_t dp = round32(kv->head_dim);
+    // Where all sequences bring as many tokens, and more rows than are split, nothing is left to the kernels of the split rows (and should a sequence
+    // have fewer after all, the others take it).
+    const bool even = rows > kSplitRows && tokens == (int64_t)kv->seqs * max_new;
+    p.few_rows = even ? 0 : kSplitRows;
+    p.rows_pad = even ? 0 : (int)std::min<int64_t>(rows, kSplitRows);
+    p.launch.tile_rows = p.rows_pad > 16 && dp <= kWideTile ? 32 : 16;
     p.launch.split_tiles = (p.rows_pad + p.launch.tile_rows - 1) / p.launch.tile_rows;
     // Four wavefronts of a workgroup take a page each; as many workgroups as the chip holds at once (two a CU), and no fewer than four pages each.
-    const int64_t tiles = pairs * p.launch.split_tiles;
+    const int64_t tiles = pairs * std::max(p.launch.split_tiles, 1);
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((512 + tiles - 1) / tiles, (pages + 3) / 4));
     p.launch.row_blocks = p.splits > 1 ? p.rows_pad : 0;
-    p.launch.page_blocks = mass && (p.splits > 1 || p.rows_pad > 16 || kv->max_pages > kMassPages) ? (int)((pages + 255) / 256) : 0;
+    p.launch.page_blocks = p.rows_pad && mass && (p.splits > 1 || p.rows_pad > 16 || kv->max_pages > kMassPages) ? (int)((pages + 255) / 256) : 0;
     p.launch.prompt_tiles = rows > kSplitRows ? (int)((rows + kTileRows - 1) / kTileRows) : 0;
-    p.launch.mass_blocks = mass && p.launch.prompt_tiles ? (int)((pages + 255) / 256) : 0;
-    // Two workgroups a CU, which have 1 KB a page each to keep a tile's weights in: at most 512 of them, and no more than 2 GB together where half are enough.
-    const size_t slot = (size_t)kv->max_pages * kTileRows * sizeof(float2);
-    p.launch.prompt_slots = p.launch.mass_blocks ? (int)std::min<int64_t>(pairs * p.launch.prompt_tiles, slot * 512 <= (size_t)2 << 30 ? 512 : 256) : 0;
+    // Row tiles that do not fill the chip share their pages out, eight at least to a workgroup.
+    const int64_t ptiles = pairs * std::max(p.launch.prompt_tiles, 1);
+    p.prompt_splits = ptiles < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / ptiles, pages / 8)) : 1;
+    p.launch.mass_blocks = mass && p.launch.prompt_tiles ? (int)((pages + (p.prompt_splits > 1 ? 3 : 255)) / (p.prompt_splits > 1 ? 4 : 256)) : 0;
+    // Workgroups that have 1 KB a page each to keep a tile's weights in: all of them where pages are shared out; else at most 512, and 256 where 512 took
+    // more than 2 GB.
+    p.slot_pages = (kv->max_pages + p.prompt_splits - 1) / p.prompt_splits;
+    const size_t slot = (size_t)p.slot_pages * kTileRows * sizeof(float2);
+    const int64_t groups = ptiles * p.prompt_splits;
+    p.launch.prompt_slots = !p.launch.mass_blocks ? 0 : (int)(p.prompt_splits > 1 ? groups : std::min<int64_t>(groups, slot * 512 <= (size_t)2 << 30 ? 512 : 256));
     size_t o = 0;
-    const size_t slots = (size_t)pairs * p.rows_pad * p.splits;
+    const size_t slots = (size_t)pairs * p.rows_pad * p.splits, rows_all = p.launch.prompt_tiles && p.prompt_splits > 1 ? (size_t)ptiles * kTileRows : 0;
     p.off_part_ml = o; o += align256(slots * sizeof(float2));
-    p.off_part_o = o; o += align256(p.splits > 1 ? slots * round32(kv->head_dim) * sizeof(float) : 0);
+    p.off_part_o = o; o += align256(p.splits > 1 ? slots * dp * sizeof(float) : 0);
     p.off_page_w = o; o += align256(mass ? (size_t)pairs * kv->max_pages * p.rows_pad * sizeof(float2) : 0);
+    p.off_prompt_ml = o; o += align256(rows_all * p.prompt_splits * sizeof(float2));
+    p.off_prompt_o = o; o += align256(rows_all * p.prompt_splits * dp * sizeof(float));
+    p.off_row_total = o; o += align256(mass ? rows_all * sizeof(float2) : 0);
     p.off_row_w = o; o += align256(slot * p.launch.prompt_slots);
-    p.off_tile_mass = o; o += align256(p.launch.mass_blocks ? (size_t)pairs * p.launch.prompt_tiles * kv->max_pages * sizeof(float) : 0);
+    p.off_tile_mass = o; o += align256(p.launch.mass_blocks && p.prompt_splits == 1 ? (size_t)ptiles * kv->max_pages * sizeof(float) : 0);
     p.total = o;
     return p;
 }
@@ -157,7 +171,7 @@ int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int he
     if (!q || !out || !workspace) return SLICER_EINVAL;
     const AttendPlan p = plan_attend(kv, heads, tokens, max_new, max_len, mass != nullptr);
     const int64_t pairs = (int64_t)kv->seqs * kv->kv_heads;
-    for (int64_t n : {(int64_t)p.launch.split_tiles * p.splits, (int64_t)p.launch.row_blocks + p.launch.page_blocks, (int64_t)p.launch.prompt_tiles, (int64_t)p.launch.mass_blocks})
+    for (int64_t n : {(int64_t)p.launch.split_tiles * p.splits, (int64_t)p.launch.row_blocks + p.launch.page_blocks, (int64_t)p.launch.prompt_tiles * (p.prompt_splits > 1 ? kTileRows : 1), (int64_t)p.launch.mass_blocks})
         if (pairs * n >= (int64_t)1 << 31) return SLICER_EINVAL;        // more workgroups than a launch can have
     KvAttendArgs a;
     a.kv = view_of(kv);
@@ -183,6 +197,12 @@ int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int he
     a.part_ml = (float2*)(ws + p.off_part_ml);
     a.part_o = (float*)(ws + p.off_part_o);
     a.page_w = (float2*)(ws + p.off_page_w);
+    a.few_rows = p.few_rows;
+    a.prompt_splits = p.prompt_splits;
+    a.slot_pages = p.slot_pages;
+    a.prompt_ml = (float2*)(ws + p.off_prompt_ml);
+    a.prompt_o = (float*)(ws + p.off_prompt_o);
+    a.row_total = (float2*)(ws + p.off_row_total);
     a.row_w = (float2*)(ws + p.off_row_w);
     a.tile_mass = (float*)(ws + p.off_tile_mass);
     return fail(dt == SLICER_F32 ? launch_kv_attend<0>(a, p.launch, (hipStream_t)hip_stream) : launch_kv_attend<1>(a, p.launch, (hipStream_t)hip_stream));

@@ -7,6 +7,8 @@
 // The tail's values are bf16 as they came and would not fit fp16: there the probabilities are split into bf16 numbers.
 #pragma once
 
+#include <type_traits>
+
 #include "slicer_kv.hpp"
 
 namespace slicer {
@@ -38,7 +40,13 @@ struct KvAttendArgs {
     float2* part_ml;
     float* part_o;
     float2* page_w;               // [sequence, head][max_pages][rows_pad] a page's sum of weights under a maximum
-    // rows that are not split, with weights: [workgroup][max_pages][128] a page's sum of a tile's rows, and [sequence, head][tiles][max_pages] of the tile
+    // other rows: sequences of at most few_rows rows a head are not looked at; with prompt_splits > 1 a row tile's pages are shared out, and [row][splits]
+    // (maximum, sum), [row][splits][dp] sums of values, [row] totals are kept; with weights [workgroup][slot_pages][128] a page's sum of a tile's
+    // rows, and [sequence, head][tiles][max_pages] of the tile
+    int few_rows, prompt_splits, slot_pages;
+    float2* prompt_ml;
+    float* prompt_o;
+    float2* row_total;
     float2* row_w;
     float* tile_mass;
 };
@@ -436,59 +444,67 @@ __device__ inline float2 kv_row_total(const float2* ml, int splits, int lane)
     return float2{M, L};
 }
 
+// A row's output from its parts, by a workgroup: all four wavefronts read parts at once, several a load (with one wavefront a row, part after part, 64 parts took
+// 64 us instead of 5).
+template <int DT, int DP>
+__device__ inline void kv_join_row(const KvAttendArgs& a, const float2* ml, const float* parts, int splits, float2 total, int64_t at, float bias, float (*xo)[DP])
+{
+    constexpr int LPP = DP / 4, PPW = kWave / LPP;       // lanes a part, parts a load (one where a part takes more than half of the lanes)
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, D = a.kv.D;
+    const int part = PPW > 1 ? lane / LPP : 0, d = (PPW > 1 ? lane % LPP : lane) * 4;
+    f32x4 v = {0, 0, 0, 0};
+    if (part < PPW && d < D) {
+#pragma unroll 4
+        for (int i = wid * PPW + part; i < splits; i += 4 * PPW) {
+            const float2 p = ml[i];
+            const f32x4 x = *(const f32x4*)(parts + (int64_t)i * DP + d) * exp2_of(p.x - total.x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += p.y != 0.0f ? x[e] : 0.0f;           // (a part without a sum was not written)
+        }
+    }
+    if constexpr (PPW > 1) {
+#pragma unroll
+        for (int q = 1; q < PPW; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float f = __shfl(v[e], (lane + q * LPP) & 63);
+                if (part == 0) v[e] += f;
+            }
+    }
+    if (part == 0 && d < DP) *(f32x4*)&xo[wid][d] = v;
+    __syncthreads();
+    if (tid * 4 < D) {
+        v = *(const f32x4*)&xo[0][tid * 4];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) v += *(const f32x4*)&xo[w][tid * 4];
+        store4<DT>(a.out, at * D + tid * 4, v * (total.y == 0.0f ? 0.0f : 1.0f / total.y));
+    }
+    if (tid == 0 && a.lse) a.lse[at] = total.y == 0.0f ? -__builtin_inff() : (total.x - bias + __log2f(total.y)) * kLn2;
+}
+
+// A row's share of a page's weight: its sum there under a maximum, the row's maximum and one over its sum.
+__device__ inline float kv_weight(float2 w, float2 row) { return w.y == 0.0f || row.y == 0.0f ? 0.0f : w.y * exp2_of(w.x - row.x) * row.y; }
+
 // What the workgroups of a split sequence left is put together: outputs, a workgroup per row, and the pages' weights, which can only be told now that
-// the rows' sums are known, a workgroup per 256 pages.  A row's parts are read by all four wavefronts at once, several parts a load: with one wavefront a row, part
-// after part, 64 parts took 64 us instead of 5.
+// the rows' sums are known, a workgroup per 256 pages.
 template <int DT, int DP>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_blocks, int page_blocks, int tile_rows)
 {
-    constexpr int LPP = DP / 4, PPW = kWave / LPP;       // lanes a part, parts a load (a part of more than 32 elements of four: one)
     __shared__ float2 xml[kSplitRows];
     __shared__ __align__(16) float xo[4][DP];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     const int blk = blockIdx.x % (row_blocks + page_blocks), bg = blockIdx.x / (row_blocks + page_blocks);
-    const int b = bg / a.kv.G, g = bg % a.kv.G, D = a.kv.D;
+    const int b = bg / a.kv.G, g = bg % a.kv.G;
     KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
     const int n_all = s.n;
     s.n = s.n < a.max_new ? s.n : a.max_new;
     const int rows = s.n * a.R;
     if (rows == 0 || rows > kSplitRows) return;
     if (blk < row_blocks) {
-        const int r = blk;
-        if (r >= rows) return;
-        const int64_t slot = ((int64_t)bg * a.rows_pad + r) * a.splits;
+        if (blk >= rows) return;
+        const int64_t slot = ((int64_t)bg * a.rows_pad + blk) * a.splits;
         const float2 ml = kv_row_total(a.part_ml + slot, a.splits, lane);
-        const int part = PPW > 1 ? lane / LPP : 0, d = (PPW > 1 ? lane % LPP : lane) * 4;
-        f32x4 v = {0, 0, 0, 0};
-        if (part < PPW && d < D) {
-#pragma unroll 4
-            for (int i = wid * PPW + part; i < a.splits; i += 4 * PPW) {
-                const float2 p = a.part_ml[slot + i];
-                const f32x4 x = *(const f32x4*)(a.part_o + (slot + i) * DP + d) * exp2_of(p.x - ml.x);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += p.y != 0.0f ? x[e] : 0.0f;       // (a part without a sum was not written)
-            }
-        }
-        if constexpr (PPW > 1) {
-#pragma unroll
-            for (int q = 1; q < PPW; ++q)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float f = __shfl(v[e], (lane + q * LPP) & 63);
-                    if (part == 0) v[e] += f;
-                }
-        }
-        if (part == 0 && d < DP) *(f32x4*)&xo[wid][d] = v;
-        __syncthreads();
-        const int64_t at = (s.first + r / a.R) * a.H + g * a.R + r % a.R;
-        const float inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
-        if (tid * 4 < D) {
-            v = *(const f32x4*)&xo[0][tid * 4];
-#pragma unroll
-            for (int w = 1; w < 4; ++w) v += *(const f32x4*)&xo[w][tid * 4];
-            store4<DT>(a.out, at * D + tid * 4, v * inv);
-        }
-        if (tid == 0 && a.lse) a.lse[at] = ml.y == 0.0f ? -__builtin_inff() : (ml.x - kPBias + __log2f(ml.y)) * kLn2;
+        kv_join_row<DT, DP>(a, a.part_ml + slot, a.part_o + slot * DP, a.splits, ml, (s.first + blk / a.R) * a.H + g * a.R + blk % a.R, kPBias, xo);
         return;
     }
     for (int r = wid; r < rows; r += 4) {
@@ -502,8 +518,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_bl
         for (int r = 0; r < rows; ++r) {
             // a row's tile came to the pages that the tile's last row sees some token of
             const int top = a.causal ? s.len - n_all + min(rows - 1, r | (tile_rows - 1)) / a.R + 1 : s.len;
-            if (p * kPage >= top || w[r].y == 0.0f) continue;
-            sum += w[r].y * exp2_of(w[r].x - xml[r].x) * xml[r].y;
+            if (p * kPage < top) sum += kv_weight(w[r], xml[r]);
         }
         float* to = a.mass + (int64_t)bg * a.kv.max_pages + p;
         *to = a.decay == 0.0f ? sum : __builtin_fmaf(*to, a.decay, sum);
@@ -515,7 +530,21 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_bl
 // Four wavefronts of 32 rows (token after token, a token's query heads of the cache head next to each other) share the pages: a page's codes are loaded one
 // page ahead, turned into bf16 and fp16 operands once for all four and read from LDS as the lanes want them.  S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16
 // products, a lane has the scores of one row.  Bound by the matrix units, the exponentials and LDS reads, in about equal parts.
+// What was measured on 8 x 2048 queries, 32 heads over 8 of 128: the pipeline of one wavefront, product by product with the vector instructions that run
+// beside it, 415 us, a page after the other 444.  With 64 rows a wavefront (half of the LDS reads, one wavefront a SIMD) 568: two
+// wavefronts hide each other's waits better than one hides its own.  A page takes a wavefront 1.33 us alone on its SIMD, two of them 2.2.
+
+
+
 constexpr int kTileRows = 128;
+
+// Share `i` of `n` of a row tile's pages.
+struct KvShare { int first, end; };
+__host__ __device__ inline KvShare kv_share(int units, int n, int i)
+{
+    const int per = (units + n - 1) / n, first = i * per < units ? i * per : units;
+    return KvShare{first, first + per < units ? first + per : units};
+}
 
 template <int DP>
 struct PromptTile {
@@ -524,24 +553,20 @@ struct PromptTile {
     static constexpr int kKeys = 2 * KK * 64 * 8, kAll = 2 * kKeys;
 };
 
-// record -> operands of 32 x 32 x 16 products in LDS (record i of 16 bytes)
+// record i of 16 bytes -> operands of 32 x 32 x 16 products in LDS: half `part` of a record of keys, word `part` of a record of values
 template <int DP>
-__device__ inline void stage_keys(uint16_t* to, int i, uint4 w)
+__device__ inline void stage_keys(uint16_t* to, int i, uint4 w, int part)
 {
     constexpr int KK = DP / 16;
     const int l = i & 63, st = i >> 6, T2 = st / (DP / 32), sl = st % (DP / 32), gq = l >> 4, cc = l & 15;
-    uint16_t* f = to + (((T2 * KK + sl * 2 + (gq >> 1)) * 64) + (gq & 1) * 32 + cc) * 8;
-    *(bf16x8*)f = codes_bf16(w.x, w.y);
-    *(bf16x8*)(f + 16 * 8) = codes_bf16(w.z, w.w);
+    *(bf16x8*)(to + (((T2 * KK + sl * 2 + (gq >> 1)) * 64) + (gq & 1) * 32 + part * 16 + cc) * 8) = part ? codes_bf16(w.z, w.w) : codes_bf16(w.x, w.y);
 }
 
 template <int DP>
-__device__ inline void stage_values(uint16_t* to, int i, uint4 w)
+__device__ inline void stage_values(uint16_t* to, int i, uint4 w, int part)
 {
     const int l = i & 63, dt = i >> 6, gq = l >> 4, cc = l & 15;
-    uint16_t* f = to + (((dt >> 1) * 4) * 64 + (gq & 1) * 32 + (dt & 1) * 16 + cc) * 8 + (gq >> 1) * 4;
-#pragma unroll
-    for (int T = 0; T < 4; ++T) *(uint2*)(f + T * 64 * 8) = codes_f16((&w.x)[T]);
+    *(uint2*)(to + (((dt >> 1) * 4 + part) * 64 + (gq & 1) * 32 + (dt & 1) * 16 + cc) * 8 + (gq >> 1) * 4) = codes_f16((&w.x)[part]);
 }
 
 // the tail: bf16 operands, nothing behind its last token
@@ -582,38 +607,40 @@ __device__ inline float other_half(float x, float* mine)             // the valu
     return __uint_as_float(r[1]);
 }
 
-// `slots`: workgroups that hold weights of a tile's rows by page on the way (a.mass), each in a part of page_w of its own.
+// `row_tiles` of 128 CT rows a head; workgroups that keep weights of a tile's rows by page on the way (a.mass) have a part of row_w each.
 template <int DT, int DP>
 __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv_prompt_kernel(KvAttendArgs a, int row_tiles)
 {
     constexpr int KK = DP / 16, DL = DP / 32, NQ = QParts<DT>::N, NP = QParts<DT>::NP, NB = QParts<DT>::NB;
     constexpr int NR = (4 * DP + 255) / 256;             // records of keys (and of values) a thread
-    constexpr int kAhead = KK < 4 ? 2 : 6;
+    constexpr int WR = 32, TR = kTileRows;               // rows of a wavefront, of the tile
     __shared__ __align__(16) uint16_t buf[2][PromptTile<DP>::kAll];
-    __shared__ float2 xrow[kTileRows];
+    __shared__ float2 xrow[TR];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 31, h = lane >> 5;
     const int heads = a.kv.seqs * a.kv.G, D = a.kv.D;
-    float2* const my_w = a.row_w + (size_t)blockIdx.x * a.kv.max_pages * kTileRows;
-    for (int64_t tile = blockIdx.x; tile < (int64_t)heads * row_tiles; tile += gridDim.x) {
+    float2* const my_w = a.row_w + (size_t)blockIdx.x * a.slot_pages * TR;
+    for (int64_t tile = blockIdx.x; tile < (int64_t)heads * row_tiles * a.prompt_splits; tile += gridDim.x) {
         // the longest tiles first; a head's tiles on one XCD (workgroup i runs on XCD i % 8), whose L2 its pages then are in
-        const int bg = (int)(tile % heads), rt = row_tiles - 1 - (int)(tile / heads);
+        const int bg = (int)(tile % heads), split = (int)(tile / heads) % a.prompt_splits, rt = row_tiles - 1 - (int)(tile / heads) / a.prompt_splits;
         const int b = bg / a.kv.G, g = bg % a.kv.G;
         KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
         const int n_all = s.n;
         s.n = s.n < a.max_new ? s.n : a.max_new;
-        const int64_t rows = (int64_t)s.n * a.R;
-        if (rows <= kSplitRows || (int64_t)rt * kTileRows >= rows) continue;
-        const int64_t rr = (int64_t)rt * kTileRows + wid * 32 + c;
-        const bool live = rr < rows;
-        const int qi = (int)((live ? rr : rows - 1) / a.R), qh = g * a.R + (int)((live ? rr : rows - 1) % a.R);
-        const int lim = !live ? 0 : a.causal ? s.len - n_all + qi + 1 : s.len;
-        const int64_t last_row = min(rows, (int64_t)(rt + 1) * kTileRows) - 1;
+        const int64_t rows = (int64_t)s.n * a.R, row0 = (int64_t)rt * TR;
+        if (rows <= a.few_rows || row0 >= rows) continue;
+        const int64_t last_row = min(rows, row0 + TR) - 1;
         const int most = a.causal ? max(0, s.len - n_all + (int)(last_row / a.R) + 1) : s.len;
-        const int least = a.causal ? s.len - n_all + (int)((int64_t)rt * kTileRows / a.R) + 1 : s.len;
-        const int full = s.len / kPage, units = (most + kPage - 1) / kPage, ufull = min(units, full);
-        const int32_t* table = a.kv.table + (int64_t)b * a.kv.max_pages;
+        const int least = a.causal ? s.len - n_all + (int)(row0 / a.R) + 1 : s.len;
+        // this workgroup's share of the pages; from here on pages are counted from its first
+        const KvShare share = kv_share((most + kPage - 1) / kPage, a.prompt_splits, split);
+        const int full = s.len / kPage - share.first, units = share.end - share.first, ufull = max(min(units, full), 0);
+        const int32_t* table = a.kv.table + (int64_t)b * a.kv.max_pages + share.first;
 
         bf16x8 q[NQ][KK];
+        const int64_t rr = row0 + wid * WR + c;
+        const bool live = rr < rows;
+        const int qi = live ? (int)(rr / a.R) : 0, qh = g * a.R + (live ? (int)(rr % a.R) : 0);
+        const int lim = (!live ? 0 : a.causal ? s.len - n_all + qi + 1 : s.len) - share.first * kPage;
         const int64_t q_at = (s.first + qi) * a.q_token + qh * a.q_head + h * 8;
 #pragma unroll
         for (int k = 0; k < KK; ++k) {
@@ -631,13 +658,13 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         for (int t = 0; t < DL; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
-
         auto rescale = [&](float f) {
 #pragma unroll
             for (int t = 0; t < DL; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[t][r] *= f;
         };
+        auto finite_max = [&]() { return m == -__builtin_inff() ? 0.0f : m; };
         auto scores = [&](const uint16_t* keys, f32x16* sc) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -652,6 +679,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                     for (int i = 0; i < NQ; ++i) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[i][k], sc[t], 0, 0, 0);
                 }
         };
+
         uint4 kb[NR], vb[NR];
         auto mine = [&](int i) { return DP % 64 == 0 || i * 256 + tid < 4 * DP; };      // whether the thread's i-th record is one
         // places and scales of 64 pages lie in the lanes
@@ -683,16 +711,16 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         };
         auto stage_k = [&](int which) {
 #pragma unroll
-            for (int i = 0; i < NR; ++i)
-                if (mine(i)) stage_keys<DP>(buf[which], i * 256 + tid, kb[i]);
+            for (int i = 0; i < 2 * NR; ++i)
+                if (mine(i >> 1)) stage_keys<DP>(buf[which], (i >> 1) * 256 + tid, kb[i >> 1], i & 1);
         };
         auto stage_v = [&](int which) {
 #pragma unroll
-            for (int i = 0; i < NR; ++i)
-                if (mine(i)) stage_values<DP>(buf[which] + PromptTile<DP>::kKeys, i * 256 + tid, vb[i]);
+            for (int i = 0; i < 4 * NR; ++i)
+                if (mine(i >> 2)) stage_values<DP>(buf[which] + PromptTile<DP>::kKeys, (i >> 2) * 256 + tid, vb[i >> 2], i & 3);
         };
-        // what page u's scores are multiplied by, and its value scale over vref with its logarithm and inverse; vref follows the scales: within
-        // 2^-6 .. 2 of a page's, so that probabilities keep their bits; less than 2^-60 of the largest counts as that (a page of zeros: any)
+        // what a page's scores are multiplied by, and its value scale over vref: its logarithm and inverse.  vref follows the scales: a page's is within
+        // 2^-6 .. 2 of it, so that probabilities keep their bits; less than 2^-60 of the largest counts as that (a page of zeros: any)
         float factor = 0.0f, lr = 0.0f, back = 1.0f;
         auto page_scales = [&](int lane_of) {
             const float ks = __uint_as_float(bcast(__float_as_uint(my_ks), lane_of)), vs = __uint_as_float(bcast(__float_as_uint(my_vs), lane_of));
@@ -700,7 +728,9 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
             vmax = fmaxf(vmax, vs);
             const float vt = fmaxf(vs, vmax * 0x1p-60f);
             if (vt > 2.0f * vref || (vs > 0.0f && vt < vref * 0.015625f)) {
-                if (vref > 0.0f) rescale(vref / vt);
+                if (vref > 0.0f) {
+                    rescale(vref / vt);
+                }
                 vref = vt;
             }
             const float ratio = vs > 0.0f ? vt * __builtin_amdgcn_rcpf(vref) : 1.0f;
@@ -723,40 +753,29 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
             if (a.mass) {
                 float here;
                 sum = other_half(sum, &here);
-                if (h == 0) my_w[(size_t)u * kTileRows + wid * 32 + c] = float2{m == -__builtin_inff() ? 0.0f : m, (sum + here) * back};
+                if (h == 0) my_w[(size_t)u * TR + wid * WR + c] = float2{finite_max(), (sum + here) * back};
             }
         };
-        // scores -> probabilities times 2^8 and the page's scale over vref; the sum goes to l
-        auto softmax = [&](f32x16* sc, int u) {
-            const int left = lim - u * kPage - h * 4;    // tokens that the row sees from the lane's first on
+        // the lane's largest score; `mask`: rows may not see the whole page
+        auto lane_max = [&](auto mask, const f32x16* sc, int u) {
+            const int left = lim - u * kPage - h * 4;
             float mx = -__builtin_inff();
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, t * 32 + (r >> 2) * 8 + (r & 3) < left ? sc[t][r] : -__builtin_inff());
-            new_maximum(mx);
-            const float off = kPromptBias + lr - (m == -__builtin_inff() ? 0.0f : m);
-            float sum = 0.0f;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    sc[t][r] = t * 32 + (r >> 2) * 8 + (r & 3) < left ? exp2_of(__builtin_fmaf(sc[t][r], factor, off)) : 0.0f;
-                    sum += sc[t][r];
-                }
-            l = __builtin_fmaf(sum, back, l);
-            page_weight(u, sum);
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, !decltype(mask)::value || t * 32 + (r >> 2) * 8 + (r & 3) < left ? sc[t][r] : -__builtin_inff());
+            return mx;
+        };
+        // a score -> the probability times 2^8 and the page's scale over vref
+        auto exponential = [&](auto mask, f32x16* sc, int e, int left, float off) {
+            float f = exp2_of(__builtin_fmaf(sc[e >> 4][e & 15], factor, off));
+            if constexpr (decltype(mask)::value) f = (e >> 4) * 32 + ((e & 15) >> 2) * 8 + (e & 3) < left ? f : 0.0f;
+            sc[e >> 4][e & 15] = f;
+            return f;
         };
         auto products = [&](const uint16_t* values, const f32x16* sc) {
-            f16x8 v[2][DL];
-#pragma unroll
-            for (int t = 0; t < DL; ++t) v[0][t] = *(const f16x8*)(values + (t * 4 * 64 + lane) * 8);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (k < 3) {
-#pragma unroll
-                    for (int t = 0; t < DL; ++t) v[(k + 1) & 1][t] = *(const f16x8*)(values + ((t * 4 + k + 1) * 64 + lane) * 8);
-                }
                 f16x8 p[NP];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -766,169 +785,138 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                     if constexpr (NP > 1) p[1][j] = (_Float16)(f - (float)hi);
                 }
 #pragma unroll
-                for (int t = 0; t < DL; ++t)
+                for (int t = 0; t < DL; ++t) {
+                    const f16x8 v = *(const f16x8*)(values + ((t * 4 + k) * 64 + lane) * 8);
 #pragma unroll
-                    for (int i = 0; i < NP; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[k & 1][t], p[i], o[t], 0, 0, 0);
+                    for (int i = 0; i < NP; ++i) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[i], o[t], 0, 0, 0);
+                }
             }
         };
 
         __syncthreads();                                 // (the tile before may still be read)
-        // Pages that every row sees whole, in a pipeline: while a page's probabilities are made and multiplied by its values, the next page's scores are
+        // The pages in a pipeline: while a page's probabilities are made and multiplied by its values, the next page's scores are
         // made, and the operands of the keys behind those and of the next values go to LDS: matrix and vector instructions of one wavefront
         // run at the same time.  Page u has its keys in buf[u % 2] one step before its values.
-        const int whole = min(ufull, max(least, 0) / kPage);
-        int u0 = 0;
-        if (whole >= 2) {
+        const int whole = min(ufull, max(least - share.first * kPage, 0) / kPage);         // pages that every row sees all of
+        if (ufull > 0) {
             int base = 0;                                // page of the lanes' first place
             fetch(0);
             load_keys(0);
             load_values(0);
             stage_k(0);
             stage_v(0);
-            load_keys(1);
+            load_keys(min(1, ufull - 1));
             stage_k(1);
             __syncthreads();
-            load_keys(min(2, whole - 1));
-            load_values(1);
+            load_keys(min(2, ufull - 1));
+            load_values(min(1, ufull - 1));
             f32x16 sa[2], sb[2];
             scores(buf[0], sa);
             __syncthreads();                             // (the first step writes the keys of page 2 there)
             page_scales(0);
-            {
-                float mx = -__builtin_inff();
+            new_maximum(lane_max(std::true_type(), sa, 0));
+            auto step = [&](auto mask, int u, f32x16* sc, f32x16* next) {
+                constexpr int NS = 4 * DL, kAhead = 4;       // operands of a page's keys, and of its values; read that far ahead
+                const uint16_t *keys = buf[(u + 1) & 1], *values = buf[u & 1] + PromptTile<DP>::kKeys;
+                uint4 op[2 * NS];
+                auto ask = [&](int i) {
+                    if (i < NS) op[i] = *(const uint4*)(keys + (((i & 1) * KK + (i >> 1)) * 64 + lane) * 8);
+                    else if (i < 2 * NS) op[i] = *(const uint4*)(values + (((i - NS) % DL * 4 + (i - NS) / DL) * 64 + lane) * 8);
+                };
+                float part[4] = {0.0f, 0.0f, 0.0f, 0.0f}, mx = -__builtin_inff();
+                const float off = kPromptBias + lr - finite_max();
+                const int left = lim - u * kPage - h * 4;
+                f16x8 p[2][NP];
+                auto narrow = [&](int k) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float f = sc[k >> 1][(k & 1) * 8 + j];
+                        const _Float16 hi = (_Float16)f;
+                        p[k & 1][0][j] = hi;
+                        if constexpr (NP > 1) p[k & 1][1][j] = (_Float16)(f - (float)hi);
+                    }
+                };
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) ask(i);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sa[t][r]);
-                new_maximum(mx);
-            }
-            auto exponentials = [&](f32x16* sc) {
-                const float off = kPromptBias + lr - (m == -__builtin_inff() ? 0.0f : m);
-                float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int r = 0; r < 16; ++r) next[t][r] = 0.0f;
+                // every product is followed by the vector instructions that run beside it, in an order that the compiler may not change (left to it, products
+                // came in a row, each behind a wait for its operand)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int i = 0; i < NS; ++i) {
+                    ask(i + kAhead);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) { sc[t][r] = exp2_of(__builtin_fmaf(sc[t][r], factor, off)); part[r & 3] += sc[t][r]; }
+                    for (int n = 0; n < NQ; ++n) next[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16_of(op[i]), q[n][i >> 1], next[i & 1], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int e = i * 32 / NS; e < (i + 1) * 32 / NS; ++e) part[e & 3] += exponential(mask, sc, e, left, off);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                narrow(0);
                 const float sum = (part[0] + part[1]) + (part[2] + part[3]);
                 l = __builtin_fmaf(sum, back, l);
-                return sum;
-            };
-            auto step = [&](int u, f32x16* sc, f32x16* next) {
-#if VAR == 3
-                __builtin_amdgcn_s_setprio(1);
-#endif
-                scores(buf[(u + 1) & 1], next);
-#if VAR == 3
-                __builtin_amdgcn_s_setprio(0);
-#endif
-                const float sum = exponentials(sc);
-#if VAR == 3
-                __builtin_amdgcn_s_setprio(1);
-#endif
-                products(buf[u & 1] + PromptTile<DP>::kKeys, sc);
-#if VAR == 3
-                __builtin_amdgcn_s_setprio(0);
-#endif
-                stage_k(u & 1);
-                stage_v((u + 1) & 1);
-                float mx = -__builtin_inff();
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int i = 0; i < NS; ++i) {
+                    const int k = i / DL, t = i % DL;
+                    ask(NS + i + kAhead);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, next[t][r]);
-                // the order of all this: operands from LDS kAhead products before they are used, the exponentials between the next page's products,
-                // conversions and what goes to LDS between this page's
-#if VAR == 2
-                __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+                    for (int n = 0; n < NP; ++n) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, op[NS + i]), p[k & 1][n], o[t], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (t == DL - 1 && k < 3) narrow(k + 1);
 #pragma unroll
-                for (int i = 0; i < 2 * KK; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, NQ, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, 64 / KK / 2, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x400, 32 / KK / 2, 0);
+                    for (int e = 0; e < 6 * NR; ++e) {       // what goes to LDS, in pieces: four of a record of values, two of a record of keys
+                        if (e * NS / (6 * NR) != i) continue;
+                        const int rec = e / 6, piece = e % 6;
+                        if (!mine(rec)) continue;
+                        if (piece < 2) stage_keys<DP>(buf[u & 1], rec * 256 + tid, kb[rec], piece);
+                        else stage_values<DP>(buf[(u + 1) & 1] + PromptTile<DP>::kKeys, rec * 256 + tid, vb[rec], piece - 2);
+                    }
+#pragma unroll
+                    for (int e = i * 32 / NS; e < (i + 1) * 32 / NS; ++e) {
+                        const int t = e / 16, r = e % 16;
+                        mx = fmaxf(mx, !decltype(mask)::value || t * 32 + (r >> 2) * 8 + (r & 3) + kPage < left ? next[t][r] : -__builtin_inff());
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-#pragma unroll
-                for (int i = 0; i < 4 * DL; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, NP, 0);
-                    if (i < 4 * DL - kAhead) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
-                }
-#elif VAR == 4
-#pragma unroll
-                for (int i = 0; i < 2 * KK; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, NQ, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x400, 32 / KK / 2, 0);
-                }
-#elif VAR == 5
-                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-                for (int i = 0; i < 2 * KK; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, NQ, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x400, 32 / KK / 2, 0);
-                }
-#elif VAR == 6
-                __builtin_amdgcn_iglp_opt(0);
-#elif VAR == 7
-                __builtin_amdgcn_iglp_opt(1);
-#endif
                 page_weight(u, sum);
                 if (u + 4 - base > 64) {                 // (places up to u + 3 are asked for below)
                     base = u;
                     fetch(u);
                 }
-                load_keys(min(u + 3, whole - 1) - base);
-                load_values(min(u + 2, whole - 1) - base);
+                load_keys(min(u + 3, ufull - 1) - base);
+                load_values(min(u + 2, ufull - 1) - base);
                 page_scales(u + 1 - base);
                 new_maximum(mx);
                 __syncthreads();
             };
             int u = 0;
             for (; u + 2 < whole; u += 2) {
-                step(u, sa, sb);
-                step(u + 1, sb, sa);
+                step(std::false_type(), u, sa, sb);
+                step(std::false_type(), u + 1, sb, sa);
             }
-            if (u + 1 < whole) {
-                step(u, sa, sb);
+            for (; u + 2 < ufull; u += 2) {
+                step(std::true_type(), u, sa, sb);
+                step(std::true_type(), u + 1, sb, sa);
+            }
+            if (u + 1 < ufull) {
+                step(std::true_type(), u, sa, sb);
                 ++u;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) sa[t] = sb[t];
             }
-            const float sum = exponentials(sa);
-            products(buf[u & 1] + PromptTile<DP>::kKeys, sa);
+            // the last page
+            const float off = kPromptBias + lr - finite_max();
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum += exponential(std::true_type(), sa, e, lim - u * kPage - h * 4, off);
+            l = __builtin_fmaf(sum, back, l);
             page_weight(u, sum);
-            u0 = whole;
-            __syncthreads();
+            products(buf[u & 1] + PromptTile<DP>::kKeys, sa);
         }
-        // the others, one at a time
-        if (u0 < ufull) {
-            fetch(u0);
-            load_keys(0);
-            load_values(0);
-            stage_k(0);
-            stage_v(0);
-        }
-        for (int u = u0; u < ufull; ++u) {
-            const int at = (u - u0) & 63;
-            page_scales(at);
-            __syncthreads();
-            if (u + 1 < ufull) {
-                if (at == 63) fetch(u + 1);
-                load_keys((at + 1) & 63);
-                load_values((at + 1) & 63);
-            }
-            const int which = (u - u0) & 1;
-            f32x16 sc[2];
-            scores(buf[which], sc);
-            softmax(sc, u);
-            products(buf[which] + PromptTile<DP>::kKeys, sc);
-            if (u + 1 < ufull) {
-                stage_k(which ^ 1);
-                stage_v(which ^ 1);
-            }
-        }
-        if (units > full) {                              // the tail
-            const int count = s.len - full * kPage;
+        if (units > max(full, 0)) {                      // the tail is in this share
+            const int count = s.len % kPage;
             __syncthreads();
             stage_tail<DP>(buf[0], buf[0] + PromptTile<DP>::kKeys, a.kv.tails + kv_tail(a.kv, b, g), count, tid);
             __syncthreads();
@@ -939,8 +927,14 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
             factor = a.scale;
             lr = 0.0f;
             back = 1.0f;
-            softmax(sc, full);
             const uint16_t* values = buf[0] + PromptTile<DP>::kKeys;
+            new_maximum(lane_max(std::true_type(), sc, full));
+            const float off = kPromptBias - finite_max();
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum += exponential(std::true_type(), sc, e, lim - full * kPage - h * 4, off);
+            l += sum;
+            page_weight(full, sum);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 bf16x8 p[NB];
@@ -964,23 +958,27 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         float here;
         l = other_half(l, &here);
         l += here;
-        const float ms = m == -__builtin_inff() ? 0.0f : m;
         if (live) {
-            const float inv = l == 0.0f ? 0.0f : vref / l;
-            const int64_t at = (s.first + qi) * a.H + qh, out_at = at * D + h * 4;
+            const int64_t at = (s.first + qi) * a.H + qh, slot = (((int64_t)bg * row_tiles + rt) * TR + wid * WR + c) * a.prompt_splits + split;
+            const float f = a.prompt_splits > 1 ? vref : l == 0.0f ? 0.0f : vref / l;
 #pragma unroll
             for (int t = 0; t < DL; ++t)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int d = t * 32 + k * 8;
-                    if (d < D - h * 4) store4<DT>(a.out, out_at + d, f32x4{o[t][k * 4], o[t][k * 4 + 1], o[t][k * 4 + 2], o[t][k * 4 + 3]} * inv);
+                    const f32x4 v = f32x4{o[t][k * 4], o[t][k * 4 + 1], o[t][k * 4 + 2], o[t][k * 4 + 3]} * f;
+                    if (a.prompt_splits > 1) *(f32x4*)(a.prompt_o + slot * DP + h * 4 + d) = v;
+                    else if (d < D - h * 4) store4<DT>(a.out, at * D + h * 4 + d, v);
                 }
-            if (h == 0 && a.lse) a.lse[at] = l == 0.0f ? -__builtin_inff() : (ms - kPromptBias + __log2f(l)) * kLn2;
+            if (h == 0) {
+                if (a.prompt_splits > 1) a.prompt_ml[slot] = float2{m, l};
+                else if (a.lse) a.lse[at] = l == 0.0f ? -__builtin_inff() : (finite_max() - kPromptBias + __log2f(l)) * kLn2;
+            }
         }
-        if (a.mass) {
+        if (a.mass && a.prompt_splits == 1) {
             // a page's sums of the tile's rows, now that the rows' own are known
-            if (h == 0) xrow[wid * 32 + c] = float2{ms, live ? 1.0f / l : 0.0f};
-            __syncthreads();
+            if (h == 0) xrow[wid * WR + c] = float2{finite_max(), live ? 1.0f / l : 0.0f};
+            __syncthreads();                             // (also for the stores to my_w)
             const float2 r0 = xrow[lane], r1 = xrow[lane + 64];
             float* to = a.tile_mass + ((int64_t)bg * row_tiles + rt) * a.kv.max_pages;
             const int pages = (s.len + kPage - 1) / kPage;
@@ -988,13 +986,13 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                 float2 w[4][2];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const size_t at = (size_t)min(p0 + e, max(units - 1, 0)) * kTileRows + lane;
-                    w[e][0] = my_w[at];
-                    w[e][1] = my_w[at + 64];
+                    const size_t from = (size_t)min(p0 + e, max(units - 1, 0)) * TR + lane;
+                    w[e][0] = my_w[from];
+                    w[e][1] = my_w[from + 64];
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float sum = (w[e][0].y == 0.0f || r0.y == 0.0f ? 0.0f : w[e][0].y * exp2_of(w[e][0].x - r0.x) * r0.y) + (w[e][1].y == 0.0f || r1.y == 0.0f ? 0.0f : w[e][1].y * exp2_of(w[e][1].x - r1.x) * r1.y);
+                    float sum = kv_weight(w[e][0], r0) + kv_weight(w[e][1], r1);
 #pragma unroll
                     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
                     if (lane == 0 && p0 + e < pages) to[p0 + e] = p0 + e < units ? sum : 0.0f;
@@ -1004,25 +1002,65 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
     }
 }
 
-// The pages' weights over the row tiles, in their order.
-__device__ inline void kv_add_tiles(const KvAttendArgs& a, int row_tiles, int page_blocks)
+// Rows of prompts whose pages were shared out (few row tiles before a long cache): a workgroup per row, as for the split rows.  With weights, the
+// rows' totals are kept for the pages' sums.
+template <int DT, int DP>
+__global__ __launch_bounds__(256) void kv_prompt_join_kernel(KvAttendArgs a, int row_tiles)
+{
+    __shared__ __align__(16) float xo[4][DP];
+    const int lane = threadIdx.x & 63;
+    const int64_t row = blockIdx.x, per_head = (int64_t)row_tiles * kTileRows;
+    const int bg = (int)(row / per_head), b = bg / a.kv.G, g = bg % a.kv.G;
+    const int64_t r = row % per_head;
+    const KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
+    const int64_t rows = (int64_t)min(s.n, a.max_new) * a.R;
+    if (rows <= a.few_rows || r >= rows) return;
+    const int64_t at = (s.first + r / a.R) * a.H + g * a.R + r % a.R;
+    const float2 ml = kv_row_total(a.prompt_ml + row * a.prompt_splits, a.prompt_splits, lane);
+    kv_join_row<DT, DP>(a, a.prompt_ml + row * a.prompt_splits, a.prompt_o + row * a.prompt_splits * DP, a.prompt_splits, ml, at, kPromptBias, xo);
+    if (threadIdx.x == 0 && a.mass) a.row_total[row] = float2{ml.x, 1.0f / ml.y};
+}
+
+// The pages' weights over the row tiles, in their order: of tiles that have summed their rows' up, or (pages shared out) over the rows, a wavefront a page.
+template <int DT>
+__global__ __launch_bounds__(256) void kv_mass_kernel(KvAttendArgs a, int row_tiles, int page_blocks)
 {
     const int bg = blockIdx.x / page_blocks, b = bg / a.kv.G;
     const KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
-    const int64_t rows = (int64_t)(s.n < a.max_new ? s.n : a.max_new) * a.R;
-    if (rows <= kSplitRows) return;
-    const int tiles = (int)((rows + kTileRows - 1) / kTileRows);
-    for (int p = blockIdx.x % page_blocks * 256 + threadIdx.x; p < (s.len + kPage - 1) / kPage; p += page_blocks * 256) {
-        const float* from = a.tile_mass + (int64_t)bg * row_tiles * a.kv.max_pages + p;
-        float sum = 0.0f;
+    const int n = min(s.n, a.max_new);
+    const int64_t rows = (int64_t)n * a.R;
+    if (rows <= a.few_rows) return;
+    const int tiles = (int)((rows + kTileRows - 1) / kTileRows), pages = (s.len + kPage - 1) / kPage;
+    float* const mass = a.mass + (int64_t)bg * a.kv.max_pages;
+    if (a.prompt_splits == 1) {
+        for (int p = blockIdx.x % page_blocks * 256 + threadIdx.x; p < pages; p += page_blocks * 256) {
+            const float* from = a.tile_mass + (int64_t)bg * row_tiles * a.kv.max_pages + p;
+            float sum = 0.0f;
 #pragma unroll 8
-        for (int t = 0; t < tiles; ++t) sum += from[(int64_t)t * a.kv.max_pages];
-        float* to = a.mass + (int64_t)bg * a.kv.max_pages + p;
-        *to = a.decay == 0.0f ? sum : __builtin_fmaf(*to, a.decay, sum);
+            for (int t = 0; t < tiles; ++t) sum += from[(int64_t)t * a.kv.max_pages];
+            mass[p] = a.decay == 0.0f ? sum : __builtin_fmaf(mass[p], a.decay, sum);
+        }
+        return;
+    }
+    const int heads = a.kv.seqs * a.kv.G, lane = threadIdx.x & 63;
+    for (int p = blockIdx.x % page_blocks * 4 + (threadIdx.x >> 6); p < pages; p += page_blocks * 4) {
+        float sum = 0.0f;
+        for (int t = 0; t < tiles; ++t) {
+            const int64_t last_row = min(rows, (int64_t)(t + 1) * kTileRows) - 1;
+            const int most = a.causal ? max(0, s.len - s.n + (int)(last_row / a.R) + 1) : s.len, units = (most + kPage - 1) / kPage;
+            if (p >= units) continue;
+            const int split = p / kv_share(units, a.prompt_splits, 0).end;
+            const size_t slot = ((size_t)(row_tiles - 1 - t) * a.prompt_splits + split) * heads + bg;
+            const float2* w = a.row_w + (slot * a.slot_pages + (p - kv_share(units, a.prompt_splits, split).first)) * kTileRows;
+            const float2* total = a.row_total + ((int64_t)bg * row_tiles + t) * kTileRows;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if ((int64_t)t * kTileRows + i * 64 + lane < rows) sum += kv_weight(w[i * 64 + lane], total[i * 64 + lane]);
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == 0) mass[p] = a.decay == 0.0f ? sum : __builtin_fmaf(mass[p], a.decay, sum);
     }
 }
-
-template <int DT>
-__global__ __launch_bounds__(256) void kv_mass_kernel(KvAttendArgs a, int row_tiles, int page_blocks) { kv_add_tiles(a, row_tiles, page_blocks); }
 
 }  // namespace slicer

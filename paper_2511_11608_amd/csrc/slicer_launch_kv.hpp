@@ -22,9 +22,9 @@ struct KvAttendLaunch {
     int tile_rows;            // rows of a tile of the sequences that are split: 16 or 32
     int split_tiles;          // their tiles
     int row_blocks, page_blocks;
-    int prompt_tiles;         // row tiles of 128; 0: no sequence can have that many rows
+    int prompt_tiles;         // row tiles of the other sequences; 0: no sequence can have that many rows
     int prompt_slots;         // workgroups that keep weights on the way
-    int mass_blocks;          // 256 pages each; 0: no weights
+    int mass_blocks;          // workgroups a head that add up weights; 0: no weights
 };
 
 template <int DT> hipError_t launch_kv_append(const KvAppendArgs& a, int64_t blocks, hipStream_t st);
@@ -72,7 +72,7 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, const KvAttendLaunch& p, hipS
     const unsigned pairs = (unsigned)(a.kv.seqs * a.kv.G);
     kv_by_size(a.kv.dp, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        {
+        if (p.split_tiles) {
             const dim3 grid(pairs * (unsigned)(p.split_tiles * a.splits));
             if (p.tile_rows == 16) hipLaunchKernelGGL((kv_split_kernel<DT, DP, 1>), grid, dim3(256), 0, st, a);
             else if constexpr (DP <= kWideTile) hipLaunchKernelGGL((kv_split_kernel<DT, DP, 2>), grid, dim3(256), 0, st, a);
@@ -80,8 +80,10 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, const KvAttendLaunch& p, hipS
                 hipLaunchKernelGGL((kv_join_kernel<DT, DP>), dim3(pairs * (unsigned)(p.row_blocks + p.page_blocks)), dim3(256), 0, st, a, p.row_blocks, p.page_blocks, p.tile_rows);
         }
         if (p.prompt_tiles) {
-            const unsigned tiles = pairs * (unsigned)p.prompt_tiles;
+            const unsigned tiles = pairs * (unsigned)(p.prompt_tiles * a.prompt_splits);
             hipLaunchKernelGGL((kv_prompt_kernel<DT, DP>), dim3(p.mass_blocks ? std::min(tiles, (unsigned)p.prompt_slots) : tiles), dim3(256), 0, st, a, p.prompt_tiles);
+            if (a.prompt_splits > 1)
+                hipLaunchKernelGGL((kv_prompt_join_kernel<DT, DP>), dim3(pairs * (unsigned)(p.prompt_tiles * kTileRows)), dim3(256), 0, st, a, p.prompt_tiles);
             if (p.mass_blocks) hipLaunchKernelGGL((kv_mass_kernel<DT>), dim3(pairs * (unsigned)p.mass_blocks), dim3(256), 0, st, a, p.prompt_tiles, p.mass_blocks);
         }
     });

@@ -230,6 +230,43 @@ def test_any_split_of_a_long_cache(max_len, dtype):
     p.check([1, 3], q, 0.2, out, lse, mass=mass, old=old)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("past,new,heads,kv_heads,dim", [([1100], [70], 2, 1, 64), ([1985], [40], 16, 2, 96), ([3000, 130], [90, 33], 4, 1, 128), ([2040], [200], 1, 1, 32), ([1600, 900], [80, 80], 8, 4, 256)])
+def test_long_cache_before_few_rows(past, new, heads, kv_heads, dim, dtype):
+    """Row tiles that do not fill the chip: their pages are shared out, the rows and weights put together behind it."""
+    torch = _torch()
+    p = Pair(len(past), kv_heads, dim, max(-(-(a + n) // PAGE) for a, n in zip(past, new)) + 2, dtype, seed=sum(past))
+    p.append(past)
+    p.append(new)
+    q = p.rand(sum(new), heads)
+    for causal in (True, False):
+        mass = torch.rand(len(past), kv_heads, p.kv.max_pages, device="cuda")
+        old = mass.clone()
+        out, lse = p.attend(new, q.cuda(), dim ** -0.5, causal, mass, decay=1.0)
+        p.check(new, q, dim ** -0.5, out, lse, causal, mass, old, 1.0)
+
+
+def test_many_tiles_give_the_same_bits_every_time():
+    """Hundreds of workgroups whose wavefronts share operands in LDS: any order of theirs gives the same result."""
+    torch = _torch()
+    p = Pair(6, 4, 128, 20, "bf16", seed=40)
+    p.append([0, 100, 64, 500, 3, 630])
+    new = [600, 511, 512, 400, 640, 577]
+    p.append(new)
+    q = p.rand(sum(new), 16).cuda()
+    first = None
+    for _ in range(12):
+        mass = torch.zeros(6, 4, 20, device="cuda")
+        out, lse = p.attend(new, q, 0.1, mass=mass)
+        got = (out.clone(), lse.clone(), mass)
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+    rows = list(range(0, 40)) + list(range(590, 600))
+    o, l, _, absv, size, allv = p.ref[0].attend(q[:600], 0.1)
+    tol = 2.0 ** -8 * np.abs(o) + (2.0 ** -11 + 2 * (144 * 2.0 ** -24 * size + 2.0 ** -22) + 700 * 2.0 ** -24)[..., None] * absv + 2.0 ** -32 * allv
+    assert (np.abs(first[0][:600].double().cpu().numpy() - o) <= tol * (1 + 2.0 ** -7))[rows].all()
+
+
 @pytest.mark.parametrize("new", [[2, 1], [40, 30]])
 def test_scores_far_below_and_above_zero(new):
     """Weights that vanish and weights that stand alone: the maximum of a part of the cache is far from the whole row's."""
