@@ -375,7 +375,7 @@ int slicer_kv_read(const slicer_kv* kv, void* k, void* v, slicer_dtype dt, int64
  *   mass          [seqs][kv_heads][max_pages]
  *   page_table_out, lens_out, mass_out   as kv->page_table, kv->lens and mass, or those very arrays (no other overlap)
  *   freed         [seqs][max_pages]: the dropped pages in their order, then -1; n_freed [seqs]: how many
- *   workspace     8 * seqs * max_pages bytes, 256-byte aligned
+ *   workspace     12 * seqs * max_pages bytes, 256-byte aligned; contents undefined before and after
  * pages, scales and tails of the handle are not looked at and may be NULL.
  * Errors: SLICER_EINVAL for negative counts or sink_pages + recent_pages > keep_pages.
  */

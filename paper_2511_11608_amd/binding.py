@@ -494,7 +494,7 @@ def alloc_kv_evict(kv: KvCache) -> KvEvicted:
     return KvEvicted(torch.empty_like(kv.page_table), torch.empty_like(kv.lens),
                      torch.empty(kv.seqs, kv.kv_heads, kv.max_pages, dtype=torch.float32, device=dev),
                      torch.empty_like(kv.page_table), torch.empty_like(kv.lens),
-                     torch.empty(8 * kv.seqs * kv.max_pages, dtype=torch.uint8, device=dev))
+                     torch.empty(12 * kv.seqs * kv.max_pages, dtype=torch.uint8, device=dev))
 
 
 def slicer_kv_evict(kv: KvCache, mass: torch.Tensor, keep_pages: int, sink_pages: int, recent_pages: int, out: KvEvicted, stream=None) -> None:
@@ -508,7 +508,7 @@ def slicer_kv_evict(kv: KvCache, mass: torch.Tensor, keep_pages: int, sink_pages
     _kv_tensor("out.mass", out.mass, torch.float32, by_head)
     _kv_tensor("out.freed", out.freed, torch.int32, table)
     _kv_tensor("out.n_freed", out.n_freed, torch.int32, (kv.seqs,))
-    if not out.workspace.is_cuda or not out.workspace.is_contiguous() or out.workspace.numel() * out.workspace.element_size() < 8 * kv.seqs * kv.max_pages:
+    if not out.workspace.is_cuda or not out.workspace.is_contiguous() or out.workspace.numel() * out.workspace.element_size() < 12 * kv.seqs * kv.max_pages:
         raise ValueError("out.workspace is too small")
     _kv_devices(kv, kv.page_table, kv.lens, mass, out.page_table, out.lens, out.mass, out.freed, out.n_freed, out.workspace)
     _check("slicer_kv_evict", load().slicer_kv_evict(

@@ -248,7 +248,20 @@ int slicer_kv_evict(const slicer_kv* kv, const float* mass, int keep_pages, int 
     a.freed = freed;
     a.n_freed = n_freed;
     a.keys = (u64*)workspace;
-    hipLaunchKernelGGL(kv_evict_kernel, dim3((unsigned)kv->seqs), dim3(1024), 0, (hipStream_t)hip_stream, a);
+    a.from = (int32_t*)(a.keys + (size_t)kv->seqs * kv->max_pages);
+    hipStream_t st = (hipStream_t)hip_stream;
+    const dim3 seqs((unsigned)kv->seqs);
+    if (kv->max_pages <= 256) {
+        hipLaunchKernelGGL(kv_evict_small_kernel<256>, seqs, dim3(256), 0, st, a);
+    } else if (kv->max_pages <= kEvictSmall) {
+        hipLaunchKernelGGL(kv_evict_small_kernel<kEvictSmall>, seqs, dim3(kEvictSmall), 0, st, a);
+    } else {
+        const int64_t blocks = (kv->max_pages + 255) / 256;
+        if (blocks * kv->seqs >= (int64_t)1 << 31) return SLICER_EINVAL;
+        hipLaunchKernelGGL(kv_evict_keys_kernel, dim3((unsigned)(blocks * kv->seqs)), dim3(256), 0, st, a, (int)blocks);
+        hipLaunchKernelGGL(kv_evict_select_kernel, seqs, dim3(1024), 0, st, a);
+        hipLaunchKernelGGL(kv_evict_move_kernel, dim3((unsigned)(kv->seqs * kv->kv_heads)), dim3(1024), 0, st, a);
+    }
     return fail(hipGetLastError());
 }
 

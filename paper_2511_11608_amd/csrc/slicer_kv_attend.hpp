@@ -816,7 +816,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
             page_scales(0);
             new_maximum(lane_max(std::true_type(), sa, 0));
             auto step = [&](auto mask, int u, f32x16* sc, f32x16* next) {
-                constexpr int NS = 4 * DL, kAhead = 4;       // operands of a page's keys, and of its values; read that far ahead
+                constexpr int NS = 4 * DL, kAhead = 3;       // operands of a page's keys, and of its values; read that far ahead
                 const uint16_t *keys = buf[(u + 1) & 1], *values = buf[u & 1] + PromptTile<DP>::kKeys;
                 uint4 op[2 * NS];
                 auto ask = [&](int i) {

@@ -1,9 +1,19 @@
 // Shrinking the attention cache: the pages with the least accumulated weight leave it (gfx950, wave64).
+//
+// Complete pages of a sequence that stay: the first `sink`, the last `recent`, and the heaviest of the others up to `keep` in all, equal weights by the
+// lower place.  A page's weight is the sum over the heads in fp64, in their order, so that its rank is that of the exact sum (fp32 sums would
+// rank near-equal pages by their rounding).  The last key that stays is found digit by digit from the highest bit in which keys differ; one ordered pass then
+// closes the gaps.  Source and destination may be the same arrays: whatever is written was read before, and nothing moves up.
+// Bound by latency: tables of up to 1024 pages take one launch, a page a thread; longer ones three, of which the first and the last, which touch the
+// weights, spread over the chip (all in one workgroup: 1 x 16384 pages of 8 heads 110 us).
 #pragma once
 
 #include "slicer_kv.hpp"
 
 namespace slicer {
+
+constexpr int kEvictSmall = 1024;         // pages
+constexpr int kEvictRun = 16;             // pages a thread at a time
 
 struct KvEvictArgs {
     const int32_t* table;
@@ -16,7 +26,8 @@ struct KvEvictArgs {
     float* out_mass;
     int32_t* freed;
     int32_t* n_freed;
-    u64* keys;                    // workspace: [seqs][max_pages]
+    u64* keys;                    // workspace, longer tables: [seqs][max_pages], then
+    int32_t* from;                // [seqs][max_pages] the place that a place's weight comes from, -1: none
 };
 
 // Order-preserving key of a sum of weights; NaN above everything.
@@ -27,102 +38,291 @@ __device__ inline u64 weight_key(double w)
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// Which complete pages of a sequence stay: the first `sink`, the last `recent`, and the heaviest of the others up to `keep` in all, equal
-// weights by the lower place.  A page's weight is the sum over the heads in fp64, in their order, so that its rank is that of the exact sum
-// (fp32 sums would rank near-equal pages by their rounding).  One workgroup a sequence: the keys once, then a most-significant-digit-first
-// selection of the last key that stays, and one ordered pass that closes the gaps.  Source and destination may be the same arrays: a chunk of pages is
-// read before it is written, and nothing moves up.
-__global__ __launch_bounds__(1024) void kv_evict_kernel(KvEvictArgs a)
+struct KvEvictRange { int len, full, lo, hi; u32 need; };      // lo .. hi - 1: pages that may go, of which `need` stay
+
+__device__ inline KvEvictRange evict_range(const KvEvictArgs& a, int b)
 {
-    constexpr int BLOCK = 1024, RB = 8;
-    __shared__ u32 hist[1 << RB];
+    KvEvictRange r;
+    const int64_t l = a.lens[b];
+    r.len = (int)(l < 0 ? 0 : l > (int64_t)a.max_pages * kPage ? (int64_t)a.max_pages * kPage : l);
+    r.full = r.len / kPage;
+    const bool over = r.full > a.keep;
+    r.lo = over ? a.sink : 0;
+    r.hi = over ? r.full - a.recent : 0;
+    r.need = over ? (u32)(a.keep - a.sink - a.recent) : 0;
+    return r;
+}
+
+__device__ inline u64 evict_key(const KvEvictArgs& a, int b, int p)
+{
+    const float* m = a.mass + (int64_t)b * a.G * a.max_pages + p;
+    double w = 0.0;
+#pragma unroll 8
+    for (int g = 0; g < a.G; ++g) w += (double)m[(int64_t)g * a.max_pages];
+    return weight_key(w);
+}
+
+struct EvictCut { u64 prefix, mask; u32 left; };               // keys above prefix under the mask stay, and the first `left` equal to it
+
+// The cut among the keys that `each` hands to its argument.  LDS: hist 2048 words, ext 2 x BLOCK / 64 of u64, scan BLOCK / 64 + 1, sel 3.
+template <int BLOCK, typename F>
+__device__ inline EvictCut evict_cut(u32 need, F each, u32* hist, u64* ext, u32* scan, u32* sel)
+{
+    constexpr int RB = 11, NW = BLOCK / kWave;
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    EvictCut cut = {0, 0, need};
+    u64 some = 0, all = ~0ull;                                 // bits set in any key, in every key
+    each([&](u64 k) { some |= k; all &= k; });
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        some |= __shfl_xor(some, o);
+        all &= __shfl_xor(all, o);
+    }
+    if (lane == 0) { ext[wid] = some; ext[NW + wid] = all; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) { some |= ext[w]; all &= ext[NW + w]; }
+    const u64 differ = some & ~all;
+    int top = differ ? 64 - __clzll((long long)differ) : 0;                     // bits from `top` on are the same in all keys,
+    const int low = differ ? __ffsll((long long)differ) - 1 : 0;               // and so are those below `low`
+    cut.mask = top >= 64 ? 0 : ~0ull << top;
+    cut.prefix = all & cut.mask;
+    while (top > low) {
+        const int shift = top > RB ? top - RB : 0, bits = top - shift;
+        for (int i = tid; i < 1 << RB; i += BLOCK) hist[i] = 0;
+        __syncthreads();
+        each([&](u64 k) {
+            if ((k & cut.mask) != cut.prefix) return;
+            // one addition for all lanes whose key falls where the first one's does: equal weights are many
+            const u32 bin = (u32)(k >> shift) & ((1u << bits) - 1), first = (u32)__builtin_amdgcn_readfirstlane((int)bin);
+            const u64 with = __ballot(bin == first);
+            if (bin != first) atomicAdd(&hist[bin], 1u);
+            else if (mask_rank(with) == 0) atomicAdd(&hist[bin], (u32)__popcll(with));
+        });
+        __syncthreads();
+        constexpr int PB = (1 << RB) / BLOCK;                  // bins a thread, from the top
+        u32 h[PB], sum = 0, total;
+#pragma unroll
+        for (int j = 0; j < PB; ++j) {
+            h[j] = hist[(1 << RB) - 1 - tid * PB - j];
+            sum += h[j];
+        }
+        u32 before = block_excl_scan<BLOCK>(sum, scan, &total);
+#pragma unroll
+        for (int j = 0; j < PB; ++j) {
+            if (before < cut.left && cut.left <= before + h[j]) { sel[0] = (u32)((1 << RB) - 1 - tid * PB - j); sel[1] = cut.left - before; sel[2] = h[j]; }
+            before += h[j];
+        }
+        __syncthreads();
+        cut.prefix |= (u64)sel[0] << shift;
+        cut.mask = shift ? ~0ull << shift : ~0ull;
+        cut.left = sel[1];
+        const bool done = sel[2] == cut.left;                  // the whole bin stays
+        __syncthreads();
+        if (done) break;
+        top = shift;
+    }
+    return cut;
+}
+
+__device__ inline bool evict_stays(const EvictCut& cut, u32 need, u64 k, u32 equals_before)
+{
+    k &= cut.mask;
+    return need && (k > cut.prefix || (k == cut.prefix && equals_before < cut.left));
+}
+
+// Up to 1024 pages: a page a thread.  Up to 256 a thread counts the keys that come before its own (66 pages: 9 us, 11 with the cut).
+template <int BLOCK>
+__global__ __launch_bounds__(BLOCK) void kv_evict_small_kernel(KvEvictArgs a)
+{
+    constexpr bool COUNT = BLOCK <= 256;
+    __shared__ u64 keys[COUNT ? BLOCK : 1];
+    __shared__ u32 hist[COUNT ? 1 : 2048];
+    __shared__ u64 ext[2 * BLOCK / kWave];
     __shared__ u32 scan[BLOCK / kWave + 1];
     __shared__ u32 sel[3];
-    const int b = blockIdx.x, tid = threadIdx.x;
-    const int64_t row = (int64_t)b * a.max_pages;
-    const float* mass = a.mass + row * a.G;
-    float* out_mass = a.out_mass + row * a.G;
-    int len = a.lens[b];
-    len = len < 0 ? 0 : len > (int64_t)a.max_pages * kPage ? a.max_pages * kPage : len;
-    const int full = len / kPage, P = a.max_pages;
-    const int lo = full > a.keep ? a.sink : 0, hi = full > a.keep ? full - a.recent : 0;       // candidates
-    u32 need = full > a.keep ? (u32)(a.keep - a.sink - a.recent) : 0;
-    u64* keys = a.keys + row;
-    for (int p = lo + tid; p < hi; p += BLOCK) {
-        double w = 0.0;
-        for (int g = 0; g < a.G; ++g) w += (double)mass[(int64_t)g * P + p];
-        keys[p] = weight_key(w);
+    const int b = blockIdx.x, p = threadIdx.x, P = a.max_pages;
+    const int64_t row = (int64_t)b * P;
+    const KvEvictRange r = evict_range(a, b);
+    const bool candidate = p >= r.lo && p < r.hi;
+    const u64 key = candidate && r.need ? evict_key(a, b, p) : 0;
+    const int id = p < P ? a.table[row + p] : -1;
+    bool stays = p < P && !candidate;
+    u32 n;
+    if constexpr (COUNT) {
+        keys[p] = key;
+        __syncthreads();
+        u32 rank = 0;
+        for (int i = r.lo; i < r.hi; ++i) rank += keys[i] > key || (keys[i] == key && i < p);
+        if (candidate) stays = rank < r.need;
+    } else {
+        EvictCut cut = {0, 0, 0};
+        if (r.need) cut = evict_cut<BLOCK>(r.need, [&](auto use) { if (candidate) use(key); }, hist, ext, scan, sel);
+        const u32 equals = block_excl_scan<BLOCK>(candidate && (key & cut.mask) == cut.prefix, scan, &n);
+        if (candidate) stays = evict_stays(cut, r.need, key, equals);
     }
-    __syncthreads();
-    // the smallest key that stays, and how many of the keys equal to it
-    u64 prefix = 0, mask = 0;
-    u32 left = need;
-    if (need) {
-        for (int shift = 64 - RB; shift >= 0; shift -= RB) {
-            for (int i = tid; i < 1 << RB; i += BLOCK) hist[i] = 0;
-            __syncthreads();
-            for (int p = lo + tid; p < hi; p += BLOCK) {
-                const u64 k = keys[p];
-                if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << RB) - 1)], 1u);
-            }
-            __syncthreads();
-            if (tid < kWave) {                                                  // from the top: 4 bins a lane
-                const int top = (1 << RB) - 1 - tid * 4;
-                u32 h[4], sum = 0;
+    const u32 before = block_excl_scan<BLOCK>(p < P && !stays, scan, &n);
+    const int to = p - (int)before;
+    if (stays) a.out_table[row + to] = id;
+    else if (p < P) a.freed[row + before] = id;
+    if (p < P && p >= P - (int)n) a.out_table[row + p] = -1;
+    if (p < P && p >= (int)n) a.freed[row + p] = -1;
+    if (p == 0) {
+        a.out_lens[b] = r.len - kPage * (int)n;
+        a.n_freed[b] = (int)n;
+    }
+    for (int g = 0; g < a.G; g += 4) {                         // four heads at a time
+        float m[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) { h[j] = hist[top - j]; sum += h[j]; }
-                u32 before = wave_scan_dpp(sum) - sum;
+        for (int i = 0; i < 4; ++i) m[i] = p < P && g + i < a.G ? a.mass[(row * a.G) + (int64_t)(g + i) * P + p] : 0.0f;
+        __syncthreads();
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (before < left && left <= before + h[j]) { sel[0] = (u32)(top - j); sel[1] = left - before; sel[2] = h[j]; }
-                    before += h[j];
-                }
-            }
-            __syncthreads();
-            prefix |= (u64)sel[0] << shift;
-            mask |= ((u64)((1u << RB) - 1)) << shift;
-            left = sel[1];
-            const bool done = sel[2] == left;                                   // the whole bin stays
-            __syncthreads();
-            if (done) break;
+        for (int i = 0; i < 4; ++i) {
+            if (g + i >= a.G || p >= P) continue;
+            float* out = a.out_mass + row * a.G + (int64_t)(g + i) * P;
+            if (stays) out[to] = m[i];
+            if (p >= P - (int)n) out[p] = 0.0f;
         }
     }
-    // pages in their order: gone, or moved up by the number of those gone before them
+}
+
+static __global__ __launch_bounds__(256) void kv_evict_keys_kernel(KvEvictArgs a, int blocks)
+{
+    const int b = blockIdx.x / blocks, p = blockIdx.x % blocks * 256 + threadIdx.x;
+    const KvEvictRange r = evict_range(a, b);
+    if (r.need && p >= r.lo && p < r.hi) a.keys[(int64_t)b * a.max_pages + p] = evict_key(a, b, p);
+}
+
+// The table of one sequence, and where its weights come from, 16384 pages at a time.  Places come from ballots, 64 pages at a time (runs of 16 pages a
+// thread, whose loads and stores touch a line a lane: 46 us for 16384 pages).
+static __global__ __launch_bounds__(1024) void kv_evict_select_kernel(KvEvictArgs a)
+{
+    constexpr int BLOCK = 1024, E = kEvictRun;
+    __shared__ u32 hist[2048];
+    __shared__ u64 ext[2 * BLOCK / kWave];
+    __shared__ u32 scan[BLOCK / kWave + 1];
+    __shared__ u32 sel[3];
+    const int b = blockIdx.x, tid = threadIdx.x, P = a.max_pages;
+    const int64_t row = (int64_t)b * P;
+    const KvEvictRange r = evict_range(a, b);
+    const u64* keys = a.keys + row;
+    EvictCut cut = {0, 0, 0};
+    if (r.need) {
+        // sixteen keys a thread; they stay in registers where that is all of them
+        u64 k[E];
+        auto load = [&](int base) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) k[e] = base + e * BLOCK + tid < r.hi ? keys[base + e * BLOCK + tid] : 0;
+        };
+        const bool once = r.hi - r.lo <= BLOCK * E;
+        if (once) load(r.lo);
+        cut = evict_cut<BLOCK>(r.need, [&](auto use) {
+            for (int base = r.lo; base < r.hi; base += BLOCK * E) {
+                if (!once) load(base);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (base + e * BLOCK + tid < r.hi) use(k[e]);
+            }
+        }, hist, ext, scan, sel);
+    }
     u32 gone_before = 0, equal_before = 0;
-    for (int base = 0; base < P; base += BLOCK) {
-        const int p = base + tid;
-        const bool candidate = p >= lo && p < hi;
-        u64 k = 0;
-        if (candidate) k = keys[p] & mask;
-        const bool equal = candidate && need && k == prefix;
-        u32 n_equal, n_gone;
-        const u32 e = block_excl_scan<BLOCK>(equal, scan, &n_equal) + equal_before;
-        const bool stays = p < P && (!candidate || (need && (k > prefix || (equal && e < left))));
-        const bool gone = p < P && !stays;
-        const u32 before = block_excl_scan<BLOCK>(gone, scan, &n_gone) + gone_before;
-        const int id = p < P ? a.table[row + p] : 0;
+    const int lane = tid & 63, wid = tid >> 6;
+    // prefix over the wavefronts of counts that are the same in all lanes of one
+    auto across = [&](u32 mine, u32* total) {
+        if (lane == 0) scan[wid] = mine;
         __syncthreads();
-        if (stays) a.out_table[row + p - before] = id;
-        if (gone) a.freed[row + before] = id;
-        for (int g = 0; g < a.G; ++g) {
-            const float m = p < P ? mass[(int64_t)g * P + p] : 0.0f;
-            __syncthreads();
-            if (stays) out_mass[(int64_t)g * P + p - before] = m;
+        u32 before = 0, sum = 0;
+#pragma unroll
+        for (int w = 0; w < BLOCK / kWave; ++w) {
+            before += w < wid ? scan[w] : 0;
+            sum += scan[w];
+        }
+        __syncthreads();
+        *total = sum;
+        return before;
+    };
+    for (int base = 0; base < P; base += BLOCK * E) {
+        const int p0 = base + wid * (kWave * E) + lane;          // a wavefront has 1024 pages, 64 at a time
+        u64 key[E], equals[E], out[E];
+        int id[E];
+        u32 count = 0, n_equal, n_gone;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = p0 + e * kWave;
+            key[e] = r.need && p >= r.lo && p < r.hi ? keys[p] : 0;
+            id[e] = p < P ? a.table[row + p] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = p0 + e * kWave;
+            equals[e] = __ballot(p >= r.lo && p < r.hi && (key[e] & cut.mask) == cut.prefix);
+            count += (u32)__popcll(equals[e]);
+        }
+        u32 at = across(count, &n_equal) + equal_before;
+        count = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = p0 + e * kWave;
+            out[e] = __ballot(p < P && p >= r.lo && p < r.hi && !evict_stays(cut, r.need, key[e], at + mask_rank(equals[e])));
+            at += (u32)__popcll(equals[e]);
+            count += (u32)__popcll(out[e]);
+        }
+        u32 before = across(count, &n_gone) + gone_before;       // (its barriers: everything here has been read)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = p0 + e * kWave;
+            const u32 rank = before + mask_rank(out[e]);
+            before += (u32)__popcll(out[e]);
+            if (p >= P) continue;
+            if (out[e] >> lane & 1u) {
+                a.freed[row + rank] = id[e];
+            } else {
+                a.out_table[row + p - rank] = id[e];
+                a.from[row + p - rank] = p;
+            }
         }
         equal_before += n_equal;
         gone_before += n_gone;
-        __syncthreads();
     }
+    __syncthreads();
     for (int p = tid; p < P; p += BLOCK) {
         if (p >= P - (int)gone_before) {
             a.out_table[row + p] = -1;
-            for (int g = 0; g < a.G; ++g) out_mass[(int64_t)g * P + p] = 0.0f;
+            a.from[row + p] = -1;
         }
         if (p >= (int)gone_before) a.freed[row + p] = -1;
     }
     if (tid == 0) {
-        a.out_lens[b] = len - kPage * (int)gone_before;
+        a.out_lens[b] = r.len - kPage * (int)gone_before;
         a.n_freed[b] = (int)gone_before;
+    }
+}
+
+// The weights of one sequence and head: 16384 places at a time are read before they are written.
+static __global__ __launch_bounds__(1024) void kv_evict_move_kernel(KvEvictArgs a)
+{
+    constexpr int BLOCK = 1024, E = kEvictRun;
+    const int b = blockIdx.x / a.G, P = a.max_pages;
+    const int32_t* from = a.from + (int64_t)b * P;
+    const float* mass = a.mass + (int64_t)blockIdx.x * P;
+    float* out = a.out_mass + (int64_t)blockIdx.x * P;
+    for (int base = 0; base < P; base += BLOCK * E) {
+        float m[E];
+        int at[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = base + e * BLOCK + threadIdx.x;
+            at[e] = p < P ? from[p] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) m[e] = at[e] >= 0 ? mass[at[e]] : 0.0f;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int p = base + e * BLOCK + threadIdx.x;
+            if (p < P) out[p] = m[e];
+        }
+        __syncthreads();
     }
 }
 

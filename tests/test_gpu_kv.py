@@ -436,7 +436,9 @@ def ref_evict(table, lens, mass, keep, sink, recent):
 @pytest.mark.parametrize("seqs,heads,pages,keep,sink,recent,kind", [
     (1, 1, 1, 0, 0, 0, "plain"), (3, 2, 9, 4, 1, 1, "plain"), (2, 8, 70, 70, 1, 4, "plain"), (5, 3, 65, 20, 0, 0, "ties"),
     (2, 4, 1500, 700, 4, 64, "ties"), (1, 8, 5000, 17, 0, 1, "plain"), (2, 2, 40, 10, 5, 5, "plain"), (2, 2, 64, 13, 2, 3, "nan"),
-    (2, 1, 300, 100, 0, 0, "equal"), (3, 12, 33, 5, 0, 2, "tiny")])
+    (2, 1, 300, 100, 0, 0, "equal"), (3, 12, 33, 5, 0, 2, "tiny"),
+    (2, 3, 256, 100, 1, 1, "ties"), (2, 2, 1024, 1000, 0, 0, "ties"), (2, 2, 1025, 3, 1, 2, "plain"), (1, 2, 40000, 30000, 4, 4, "ties"), (2, 1, 17000, 16500, 0, 0, "equal"),
+    (2, 2, 2000, 30, 5, 5, "nan"), (1, 3, 3000, 0, 0, 0, "plain"), (2, 12, 1500, 700, 0, 2, "tiny")])
 def test_evict(seqs, heads, pages, keep, sink, recent, kind, in_place):
     torch = _torch()
     from paper_2511_11608_amd import binding
