@@ -360,21 +360,30 @@ class KvCache:
     def __init__(self, pages, scales, tails, page_table, lens, seqs, kv_heads, head_dim, n_pages, max_pages):
         self.pages, self.scales, self.tails, self.page_table, self.lens = pages, scales, tails, page_table, lens
         self.seqs, self.kv_heads, self.head_dim, self.n_pages, self.max_pages = seqs, kv_heads, head_dim, n_pages, max_pages
-        self._c, self._key = None, None
+        self._c, self._key, self._held, self._need = None, None, (), (None, 0)
 
     def c(self) -> SlicerKv:
-        """The C handle of the tensors as they are now."""
+        """The C handle of the tensors as they are now; they are checked when one of them or a size is another than before."""
+        t = (self.pages, self.scales, self.tails, self.page_table, self.lens)
         key = (self.pages.data_ptr(), self.scales.data_ptr(), self.tails.data_ptr(), self.page_table.data_ptr(), self.lens.data_ptr(),
                self.seqs, self.kv_heads, self.head_dim, self.max_pages, self.n_pages)
-        if key != self._key:
-            _kv_tensor("page_table", self.page_table, torch.int32, (self.seqs, self.max_pages))
-            _kv_tensor("lens", self.lens, torch.int32, (self.seqs,))
+        if key != self._key or any(a is not b for a, b in zip(t, self._held)):
+            dev = self.pages.get_device()
+            _kv_tensor("page_table", self.page_table, torch.int32, (self.seqs, self.max_pages), dev)
+            _kv_tensor("lens", self.lens, torch.int32, (self.seqs,), dev)
             sizes = _kv_sizes(SlicerKv(None, None, None, None, None, *key[5:]))
-            for name, t, size in zip(("pages", "scales", "tails"), (self.pages, self.scales, self.tails), sizes):
-                if not t.is_cuda or not t.is_contiguous() or t.numel() * t.element_size() < size:
-                    raise ValueError(f"{name} must be a contiguous tensor of {size} bytes on the GPU")
-            self._c, self._key = SlicerKv(*key), key
+            for name, x, size in zip(("pages", "scales", "tails"), t, sizes):
+                _kv_bytes(name, x, size, dev)
+            self._c, self._key, self._held, self._need = SlicerKv(*key), key, t, (None, 0)
         return self._c
+
+    def workspace_bytes(self, c, *shape) -> int:
+        """slicer_kv_attend_sizes for heads, tokens, max_new, max_len, with_mass."""
+        if self._need[0] != shape:
+            w = C.c_size_t(0)
+            _check("slicer_kv_attend_sizes", load().slicer_kv_attend_sizes(C.byref(c), *shape, C.byref(w)))
+            self._need = (shape, w.value)
+        return self._need[1]
 
 
 class KvEvicted:
@@ -384,9 +393,14 @@ class KvEvicted:
         self.page_table, self.lens, self.mass, self.freed, self.n_freed, self.workspace = page_table, lens, mass, freed, n_freed, workspace
 
 
-def _kv_tensor(name: str, t: torch.Tensor, dtype, shape) -> None:
-    if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on the GPU")
+def _kv_tensor(name: str, t: torch.Tensor, dtype, shape, dev: int) -> None:
+    if t.get_device() != dev or dev < 0 or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on the cache's GPU")
+
+
+def _kv_bytes(name: str, t: torch.Tensor, size: int, dev: int) -> None:
+    if t.get_device() != dev or dev < 0 or not t.is_contiguous() or t.numel() * t.element_size() < size:
+        raise ValueError(f"{name} must be a contiguous tensor of {size} bytes on the cache's GPU")
 
 
 def _kv_sizes(c: SlicerKv):
@@ -409,35 +423,26 @@ def alloc_kv(seqs: int, kv_heads: int, head_dim: int, n_pages: int, max_pages: i
                    seqs, kv_heads, head_dim, n_pages, max_pages)
 
 
-def _kv_rows(name: str, x: torch.Tensor, heads: int, head_dim: int, device) -> None:
-    if not x.is_cuda or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim or x.device != device:
-        raise ValueError(f"{name} must be a [tokens, {heads}, {head_dim}] tensor on the cache's GPU")
-    if x.stride(2) != 1 and head_dim > 1:
-        raise ValueError(f"{name}: the elements of a head must lie next to each other")
+def _kv_rows(name: str, x: torch.Tensor, heads: int, head_dim: int, dev: int) -> None:
+    if x.get_device() != dev or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim or (x.stride(2) != 1 and x.shape[0]):
+        raise ValueError(f"{name} must be a [tokens, {heads}, {head_dim}] tensor on the cache's GPU, the elements of a head next to each other")
 
 
 def _kv_call(kv: KvCache, starts: torch.Tensor):
-    c = kv.c()
-    _kv_tensor("starts", starts, torch.int32, (kv.seqs + 1,))
-    _kv_devices(kv, kv.scales, kv.tails, kv.page_table, kv.lens, starts)
-    return c
-
-
-def _kv_devices(kv: KvCache, *tensors) -> None:
-    """Kernels go to the current device: everything has to be there."""
-    here = torch._C._cuda_getDevice()
-    if kv.pages.device.index != here:
+    """The handle and the device of a call: kernels go to the current device, everything has to be there."""
+    c, dev = kv.c(), kv.pages.get_device()
+    if starts is not None:
+        _kv_tensor("starts", starts, torch.int32, (kv.seqs + 1,), dev)
+    if dev != torch._C._cuda_getDevice():
         raise ValueError("the cache is not on the current device")
-    for t in tensors:
-        if t is not None and t.device != kv.pages.device:
-            raise ValueError("tensors of one call must be on one device")
+    return c, dev
 
 
 def slicer_kv_append(kv: KvCache, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, max_new: int, stream=None) -> None:
     """Takes the tokens k, v [tokens, kv_heads, head_dim] into the cache; rows starts[i]..starts[i+1] are the last tokens of sequence i's lens[i]."""
-    c = _kv_call(kv, starts)
-    _kv_rows("k", k, kv.kv_heads, kv.head_dim, kv.pages.device)
-    _kv_rows("v", v, kv.kv_heads, kv.head_dim, kv.pages.device)
+    c, dev = _kv_call(kv, starts)
+    _kv_rows("k", k, kv.kv_heads, kv.head_dim, dev)
+    _kv_rows("v", v, kv.kv_heads, kv.head_dim, dev)
     if k.shape[0] != v.shape[0] or k.dtype != v.dtype:
         raise ValueError("k and v must have the same type and number of tokens")
     _check("slicer_kv_append", load().slicer_kv_append(C.byref(c), k.data_ptr(), v.data_ptr(), _dt_of(k), k.shape[0], starts.data_ptr(), max_new,
@@ -446,9 +451,7 @@ def slicer_kv_append(kv: KvCache, k: torch.Tensor, v: torch.Tensor, starts: torc
 
 def slicer_kv_attend_sizes(kv: KvCache, heads: int, tokens: int, max_new: int, max_len: int, with_mass: bool = True) -> int:
     """Workspace bytes of slicer_kv_attend, with `mass` or without."""
-    w = C.c_size_t(0)
-    _check("slicer_kv_attend_sizes", load().slicer_kv_attend_sizes(C.byref(kv.c()), heads, tokens, max_new, max_len, int(with_mass), C.byref(w)))
-    return w.value
+    return kv.workspace_bytes(kv.c(), heads, tokens, max_new, max_len, int(with_mass))
 
 
 def alloc_kv_workspace(kv: KvCache, heads: int, tokens: int, max_new: int, max_len: int, with_mass: bool = True) -> torch.Tensor:
@@ -459,21 +462,16 @@ def slicer_kv_attend(kv: KvCache, q: torch.Tensor, starts: torch.Tensor, max_new
                      workspace: torch.Tensor, lse=None, mass=None, mass_decay: float = 0.0, causal: bool = True, stream=None) -> None:
     """Attention of the queries q [tokens, heads, head_dim] over the cache, whose last tokens are theirs; workspace from alloc_kv_workspace with the
     same numbers.  lse [tokens, heads] and mass [seqs, kv_heads, max_pages] (fp32) are optional outputs."""
-    c = _kv_call(kv, starts)
+    c, dev = _kv_call(kv, starts)
     tokens, heads = q.shape[0], q.shape[1] if q.dim() == 3 else 0
-    _kv_rows("q", q, heads, kv.head_dim, kv.pages.device)
-    _kv_tensor("out", out, q.dtype, q.shape)
+    _kv_rows("q", q, heads, kv.head_dim, dev)
+    _kv_tensor("out", out, q.dtype, q.shape, dev)
     if lse is not None:
-        _kv_tensor("lse", lse, torch.float32, (tokens, heads))
+        _kv_tensor("lse", lse, torch.float32, (tokens, heads), dev)
     if mass is not None:
-        _kv_tensor("mass", mass, torch.float32, (kv.seqs, kv.kv_heads, kv.max_pages))
-    L = load()
-    need = C.c_size_t(0)
-    _check("slicer_kv_attend_sizes", L.slicer_kv_attend_sizes(C.byref(c), heads, tokens, max_new, max_len, int(mass is not None), C.byref(need)))
-    if not workspace.is_cuda or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need.value:
-        raise ValueError(f"workspace must be a contiguous tensor of {need.value} bytes on the GPU")
-    _kv_devices(kv, out, lse, mass, workspace)
-    _check("slicer_kv_attend", L.slicer_kv_attend(
+        _kv_tensor("mass", mass, torch.float32, (kv.seqs, kv.kv_heads, kv.max_pages), dev)
+    _kv_bytes("workspace", workspace, kv.workspace_bytes(c, heads, tokens, max_new, max_len, int(mass is not None)), dev)
+    _check("slicer_kv_attend", load().slicer_kv_attend(
         C.byref(c), q.data_ptr(), _dt_of(q), heads, tokens, starts.data_ptr(), max_new, max_len, q.stride(0), q.stride(1), scale, int(causal),
         out.data_ptr(), lse.data_ptr() if lse is not None else None, mass.data_ptr() if mass is not None else None, mass_decay,
         workspace.data_ptr(), _stream_handle(stream)))
@@ -481,10 +479,9 @@ def slicer_kv_attend(kv: KvCache, q: torch.Tensor, starts: torch.Tensor, max_new
 
 def slicer_kv_read(kv: KvCache, starts: torch.Tensor, max_new: int, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
     """Rows starts[i].. of k and v [tokens, kv_heads, head_dim] get the first tokens of sequence i."""
-    c = _kv_call(kv, starts)
-    _kv_tensor("k", k, k.dtype, (k.shape[0], kv.kv_heads, kv.head_dim))
-    _kv_tensor("v", v, k.dtype, k.shape)
-    _kv_devices(kv, k, v)
+    c, dev = _kv_call(kv, starts)
+    _kv_tensor("k", k, k.dtype, (k.shape[0], kv.kv_heads, kv.head_dim), dev)
+    _kv_tensor("v", v, k.dtype, k.shape, dev)
     _check("slicer_kv_read", load().slicer_kv_read(C.byref(c), k.data_ptr(), v.data_ptr(), _dt_of(k), k.shape[0], starts.data_ptr(), max_new,
                                                    _stream_handle(stream)))
 
@@ -500,17 +497,15 @@ def alloc_kv_evict(kv: KvCache) -> KvEvicted:
 def slicer_kv_evict(kv: KvCache, mass: torch.Tensor, keep_pages: int, sink_pages: int, recent_pages: int, out: KvEvicted, stream=None) -> None:
     """Drops the full pages with the least mass where a sequence has more than keep_pages.  `out` gets the tables that follow (its page_table, lens and
     mass may be the cache's and `mass` themselves)."""
-    c = kv.c()
+    c, dev = _kv_call(kv, None)
     table, by_head = (kv.seqs, kv.max_pages), (kv.seqs, kv.kv_heads, kv.max_pages)
-    _kv_tensor("mass", mass, torch.float32, by_head)
-    _kv_tensor("out.page_table", out.page_table, torch.int32, table)
-    _kv_tensor("out.lens", out.lens, torch.int32, (kv.seqs,))
-    _kv_tensor("out.mass", out.mass, torch.float32, by_head)
-    _kv_tensor("out.freed", out.freed, torch.int32, table)
-    _kv_tensor("out.n_freed", out.n_freed, torch.int32, (kv.seqs,))
-    if not out.workspace.is_cuda or not out.workspace.is_contiguous() or out.workspace.numel() * out.workspace.element_size() < 12 * kv.seqs * kv.max_pages:
-        raise ValueError("out.workspace is too small")
-    _kv_devices(kv, kv.page_table, kv.lens, mass, out.page_table, out.lens, out.mass, out.freed, out.n_freed, out.workspace)
+    _kv_tensor("mass", mass, torch.float32, by_head, dev)
+    _kv_tensor("out.page_table", out.page_table, torch.int32, table, dev)
+    _kv_tensor("out.lens", out.lens, torch.int32, (kv.seqs,), dev)
+    _kv_tensor("out.mass", out.mass, torch.float32, by_head, dev)
+    _kv_tensor("out.freed", out.freed, torch.int32, table, dev)
+    _kv_tensor("out.n_freed", out.n_freed, torch.int32, (kv.seqs,), dev)
+    _kv_bytes("out.workspace", out.workspace, 12 * kv.seqs * kv.max_pages, dev)
     _check("slicer_kv_evict", load().slicer_kv_evict(
         C.byref(c), mass.data_ptr(), keep_pages, sink_pages, recent_pages, out.page_table.data_ptr(), out.lens.data_ptr(), out.mass.data_ptr(),
         out.freed.data_ptr(), out.n_freed.data_ptr(), out.workspace.data_ptr(), _stream_handle(stream)))
