@@ -302,7 +302,7 @@ int slicer_stream_words(const void* meta, uint64_t* words, void* hip_stream);
  *            that is not full yet are held so, in the sequence's tail.  When a page gets full its 64 x head_dim keys of a head are held as
  *            code * scale, with amax their largest magnitude: scale = amax / 127, code = rint(x * (127 / amax)) within -127..127, every step one fp32
  *            operation; values likewise, with a scale of their own.  amax < 2^-119: zeros.  The result does not depend on how many tokens a call brings.
- *   values   finite, magnitudes up to 2^100.  A token with others is held as a key of NaN and a value of zero, in a full page as zeros under a key scale of
+ *   values   queries, keys and values finite, magnitudes up to 2^100.  A token with others is held as a key of NaN and a value of zero, in a full page as zeros under a key scale of
  *            NaN: outputs of queries that see it (in a full page: that see the page) are NaN, no others are touched.
  *   handle   slicer_kv is read on the host during a call; its pointers are device memory of the caller, 256-byte aligned, sizes from slicer_kv_sizes.
  *            pages, scales and tails need no initial values.  page_table and lens are the caller's to keep, on the device; entries that
@@ -310,12 +310,13 @@ int slicer_stream_words(const void* meta, uint64_t* words, void* hip_stream);
  *            if within [0, 64 max_pages], starts as if within [0, tokens].
  *   batches  a call's new tokens (queries) of sequence i are rows starts[i] .. starts[i + 1] - 1 of [tokens][heads][head_dim] tensors (device array, seqs + 1
  *            entries); a sequence may have none.  Rows outside every sequence are left as they were.  lens[i] counts the sequence's tokens with the call's new ones.
- *            max_new: no sequence has more new tokens (those of a longer one are left out).
+ *            max_new: no sequence has more new tokens (of a longer one, slicer_kv_attend leaves the queries behind them out).
  * dt is the type of k, v, q and out; softmax, sums and weights are fp32.  All calls but slicer_kv_sizes and slicer_kv_attend_sizes, which are host
  * computations, are asynchronous on hip_stream, allocate nothing and can be captured into a HIP graph.  Calls that share a workspace, or of
  * which one writes what another reads, must be ordered by the caller; others may overlap.
  * Errors: SLICER_EINVAL for null pointers, seqs, heads, max_pages or n_pages < 1 (max_pages > 2^24, n_pages >= 2^31, seqs * kv_heads >= 2^22),
- * head_dim no multiple of 8 in 8..256, max_new < 1 with tokens > 0, negative tokens, and what the calls name; SLICER_EUNSUPPORTED for an unknown dtype.
+ * head_dim no multiple of 8 in 8..256, max_new < 1 with tokens > 0, tokens outside [0, 2^31), buffers off a 16-byte boundary, more than 2^24 workgroups,
+ * and what the calls name; SLICER_EUNSUPPORTED for an unknown dtype.
  */
 #define SLICER_KV_PAGE 64
 
@@ -346,7 +347,7 @@ int slicer_kv_append(const slicer_kv* kv, const void* k, const void* v, slicer_d
  * query's own token is the last one it sees) or all lens tokens; out = sum softmax(scale * q . key) value.  A query that sees none gets zeros.
  *   q          [tokens][heads][head_dim], element stride 1, strides q_token, q_head in elements
  *   heads      a multiple of kv_heads
- *   out        [tokens][heads][head_dim], contiguous; may not overlap q
+ *   out        [tokens][heads][head_dim], contiguous, 16-byte aligned; may not overlap q
  *   lse        [tokens][heads] fp32 or NULL: log of the sum of exp(scale * q . key); -inf for a query that sees nothing
  *   mass       [seqs][kv_heads][max_pages] fp32 or NULL: mass = mass_decay * mass + the sum of the probabilities that the page's tokens got from the
  *              call's queries in the kv head's query heads, for the pages that hold tokens of sequences with new ones; others stay.  mass_decay in [0, 1]; with 0

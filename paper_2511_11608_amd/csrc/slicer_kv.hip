@@ -30,6 +30,7 @@ int check_call(const slicer_kv* kv, int dt, int64_t tokens, const int32_t* start
     if (rc) return rc;
     if (dt != SLICER_F32 && dt != SLICER_BF16) return SLICER_EUNSUPPORTED;
     if (!kv->pages || !kv->scales || !kv->tails || !kv->page_table || !kv->lens) return SLICER_EINVAL;
+    if (((uintptr_t)kv->pages | (uintptr_t)kv->scales | (uintptr_t)kv->tails) & 15) return SLICER_EINVAL;      // read 16 bytes at a time
     if (tokens < 0 || tokens >= (int64_t)1 << 31 || (tokens > 0 && (!starts || max_new < 1))) return SLICER_EINVAL;
     return SLICER_OK;
 }
@@ -58,7 +59,11 @@ bool wide_rows(const void* p, int dt, int64_t token, int64_t head)
     return ((uintptr_t)p & 15) == 0 && token % e == 0 && head % e == 0;
 }
 
-int64_t blocks_of(int64_t tokens, int max_new) { return (std::min<int64_t>(tokens, max_new) + kPage - 2) / kPage + 1; }
+// Blocks of 64 token places that a sequence's new tokens can touch; the kernels go round where a launch cannot have as many.
+int64_t blocks_of(int64_t tokens, int max_new) { return std::min<int64_t>((std::min<int64_t>(tokens, max_new) + kPage - 2) / kPage + 1, 65536); }
+
+// Workgroups of 256 threads in one dimension of a launch (which counts threads in 32 bits).
+constexpr int64_t kMaxGroups = (int64_t)1 << 24;
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
@@ -168,11 +173,11 @@ int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int he
     if (rc) return rc;
     if (heads < 1 || heads % kv->kv_heads || !std::isfinite(scale) || !(mass_decay >= 0.0 && mass_decay <= 1.0) || max_len < 0) return SLICER_EINVAL;
     if (tokens == 0) return SLICER_OK;
-    if (!q || !out || !workspace) return SLICER_EINVAL;
+    if (!q || !out || !workspace || (((uintptr_t)out | (uintptr_t)workspace) & 15)) return SLICER_EINVAL;
     const AttendPlan p = plan_attend(kv, heads, tokens, max_new, max_len, mass != nullptr);
     const int64_t pairs = (int64_t)kv->seqs * kv->kv_heads;
     for (int64_t n : {(int64_t)p.launch.split_tiles * p.splits, (int64_t)p.launch.row_blocks + p.launch.page_blocks, (int64_t)p.launch.prompt_tiles * (p.prompt_splits > 1 ? kTileRows : 1), (int64_t)p.launch.mass_blocks})
-        if (pairs * n >= (int64_t)1 << 31) return SLICER_EINVAL;        // more workgroups than a launch can have
+        if (pairs * n >= kMaxGroups) return SLICER_EINVAL;        // more workgroups than a launch can have
     KvAttendArgs a;
     a.kv = view_of(kv);
     a.q = q;
@@ -230,7 +235,7 @@ int slicer_kv_evict(const slicer_kv* kv, const float* mass, int keep_pages, int 
 {
     int rc = check_kv(kv);
     if (rc) return rc;
-    if (!kv->page_table || !kv->lens || !mass || !page_table_out || !lens_out || !mass_out || !freed || !n_freed || !workspace) return SLICER_EINVAL;
+    if (!kv->page_table || !kv->lens || !mass || !page_table_out || !lens_out || !mass_out || !freed || !n_freed || !workspace || ((uintptr_t)workspace & 15)) return SLICER_EINVAL;
     if (keep_pages < 0 || sink_pages < 0 || recent_pages < 0 || (int64_t)sink_pages + recent_pages > keep_pages) return SLICER_EINVAL;
     KvEvictArgs a;
     a.table = kv->page_table;
@@ -257,7 +262,7 @@ int slicer_kv_evict(const slicer_kv* kv, const float* mass, int keep_pages, int 
         hipLaunchKernelGGL(kv_evict_small_kernel<kEvictSmall>, seqs, dim3(kEvictSmall), 0, st, a);
     } else {
         const int64_t blocks = (kv->max_pages + 255) / 256;
-        if (blocks * kv->seqs >= (int64_t)1 << 31) return SLICER_EINVAL;
+        if (blocks * kv->seqs >= kMaxGroups) return SLICER_EINVAL;
         hipLaunchKernelGGL(kv_evict_keys_kernel, dim3((unsigned)(blocks * kv->seqs)), dim3(256), 0, st, a, (int)blocks);
         hipLaunchKernelGGL(kv_evict_select_kernel, seqs, dim3(1024), 0, st, a);
         hipLaunchKernelGGL(kv_evict_move_kernel, dim3((unsigned)(kv->seqs * kv->kv_heads)), dim3(1024), 0, st, a);

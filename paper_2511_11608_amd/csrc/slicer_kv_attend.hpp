@@ -136,7 +136,7 @@ __global__ __launch_bounds__(256, (QT == 1 && DP <= 160) || (QT == 1 && DP == 19
     KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
     const int n_all = s.n;
     s.n = s.n < a.max_new ? s.n : a.max_new;
-    const int rows = s.n * a.R;
+    const int rows = (int)min((int64_t)s.n * a.R, (int64_t)kSplitRows + 1);
     if (rt * TR >= rows || rows > kSplitRows) return;
     int lim[QT];                                         // tokens that the lane's rows see
 #pragma unroll
@@ -498,7 +498,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_bl
     KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
     const int n_all = s.n;
     s.n = s.n < a.max_new ? s.n : a.max_new;
-    const int rows = s.n * a.R;
+    const int rows = (int)min((int64_t)s.n * a.R, (int64_t)kSplitRows + 1);
     if (rows == 0 || rows > kSplitRows) return;
     if (blk < row_blocks) {
         if (blk >= rows) return;

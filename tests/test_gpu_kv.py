@@ -96,7 +96,7 @@ class Pair:
             if got_l is not None:
                 assert np.array_equal(np.isnan(l), np.isnan(got_l)) and np.array_equal(np.isneginf(l), np.isneginf(got_l)), i
                 fl = np.isfinite(l)
-                assert (np.abs(got_l - l)[fl] <= (delta + (len(r) + 64) * 2.0 ** -24 + 2.0 ** -22 * np.abs(l))[fl]).all(), i
+                assert (np.abs(got_l[fl] - l[fl]) <= (delta + (len(r) + 64) * 2.0 ** -24 + 2.0 ** -22 * np.abs(l))[fl]).all(), i
             if mass is not None:
                 g = mass[i].double().cpu().numpy()
                 was = old[i].double().cpu().numpy()
@@ -171,9 +171,10 @@ def test_pages_of_unusual_values(kind):
     p.b.slicer_kv_read(p.kv, starts_of([128]), 128, k, v)
     wk, wv, _ = p.ref[0].values()
     assert torch.equal(k.cpu(), torch.tensor(wk).float()) and torch.equal(v.cpu(), torch.tensor(wv).float())
-    q = p.rand(1, 1, 2.0 ** -100 if kind == "huge" else 1.0)
-    out, lse = p.attend([1], q.cuda(), 0.125)
-    p.check([1], q, 0.125, out, lse)
+    for n in (1, 90):                                     # as split rows and as a prompt's
+        q = p.rand(n, 1, 2.0 ** -100 if kind == "huge" else 1.0)
+        out, lse = p.attend([n], q.cuda(), 0.125)
+        p.check([n], q, 0.125, out, lse)
 
 
 SHAPES = [

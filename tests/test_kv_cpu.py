@@ -71,11 +71,18 @@ def test_null_pointers_types_and_counts_are_refused(lib):
         assert call(lib, kv, tokens=-1) == -1 and call(lib, kv, tokens=1 << 31) == -1
         assert call(lib, kv, max_new=0) == -1 and call(lib, kv, starts=None) == -1
         assert call(lib, kv, tokens=0, starts=None, max_new=0) == 0                       # nothing to do
+    for name in ("pages", "scales", "tails"):
+        for call in (append, attend, read):
+            assert call(lib, handle(**{name: 264})) == -1, name                           # 16-byte loads
+    assert attend(lib, kv, out=264) == -1 and attend(lib, kv, ws=264) == -1 and evict(lib, kv, ws=264) == -1
     assert append(lib, kv, k=None) == -1 and append(lib, kv, v=None) == -1 and read(lib, kv, k=None) == -1 and read(lib, kv, v=None) == -1
     assert attend(lib, kv, q=None) == -1 and attend(lib, kv, out=None) == -1 and attend(lib, kv, ws=None) == -1
     assert attend(lib, kv, heads=0) == -1 and attend(lib, kv, heads=6) == -1 and attend(lib, kv, max_len=-1) == -1
     for scale in (float("nan"), float("inf")):
         assert attend(lib, kv, scale=scale) == -1
+    # more workgroups than a launch can have
+    assert attend(lib, handle(seqs=1 << 12, kv_heads=512), heads=512 * 512, tokens=1 << 20, max_new=1 << 10) == -1
+    assert evict(lib, handle(seqs=1 << 20, kv_heads=1, max_pages=1 << 16)) == -1
     for decay in (-0.1, 1.1, float("nan")):
         assert attend(lib, kv, decay=decay) == -1
     assert evict(lib, kv, mass=None) == -1 and evict(lib, kv, ws=None) == -1
