@@ -892,6 +892,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                 __syncthreads();
             };
             int u = 0;
+            // (a choice between the two for every page had the compiler put 744 bytes a lane into scratch memory: 1860 us instead of 400)
             for (; u + 2 < whole; u += 2) {
                 step(std::false_type(), u, sa, sb);
                 step(std::false_type(), u + 1, sb, sa);
@@ -960,13 +961,13 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         l += here;
         if (live) {
             const int64_t at = (s.first + qi) * a.H + qh, slot = (((int64_t)bg * row_tiles + rt) * TR + wid * WR + c) * a.prompt_splits + split;
-            const float f = a.prompt_splits > 1 ? vref : l == 0.0f ? 0.0f : vref / l;
+            const float f = a.prompt_splits > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;      // (not times vref at once: that may leave fp32's normal range)
 #pragma unroll
             for (int t = 0; t < DL; ++t)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int d = t * 32 + k * 8;
-                    const f32x4 v = f32x4{o[t][k * 4], o[t][k * 4 + 1], o[t][k * 4 + 2], o[t][k * 4 + 3]} * f;
+                    const f32x4 v = f32x4{o[t][k * 4], o[t][k * 4 + 1], o[t][k * 4 + 2], o[t][k * 4 + 3]} * f * vref;
                     if (a.prompt_splits > 1) *(f32x4*)(a.prompt_o + slot * DP + h * 4 + d) = v;
                     else if (d < D - h * 4) store4<DT>(a.out, at * D + h * 4 + d, v);
                 }

@@ -1,7 +1,7 @@
 """The attention cache in 8 bits on the GPU (slicer_kv_*), against its definition in 64 bits (tests/kv_ref.py).
 
 Tolerances.  What the cache holds is compared bit for bit.  An output is off by
-  half a step of its type,
+  half a step of its type (which below the smallest normal number is that number's),
   the rounding of the probabilities: fp16, half a step 2^-11 of each (bf16 outputs); two fp16 numbers for fp32 outputs, 2^-22 of each and
   less than that again where the second is below fp16's smallest normal number,
   the scores' error delta: D products summed in fp32, and scale, maximum and exponential after it, (D + 16) 2^-24 of sum |q k| scale, plus 2^-22 from
@@ -89,7 +89,8 @@ class Pair:
             at += n
             delta = (D + 16) * 2.0 ** -24 * size + 2.0 ** -22
             p_bits = 2.0 ** -11 if q.dtype == torch.bfloat16 else 2.0 ** -21
-            tol = torch.finfo(q.dtype).eps / 2 * (1 + 2.0 ** -7) * np.abs(o) + (p_bits + 2 * delta + (len(r) + 64) * 2.0 ** -24)[..., None] * absv + 2.0 ** -32 * allv
+            fi = torch.finfo(q.dtype)
+            tol = fi.eps / 2 * (1 + 2.0 ** -7) * np.abs(o) + fi.eps / 2 * fi.smallest_normal + (p_bits + 2 * delta + (len(r) + 64) * 2.0 ** -24)[..., None] * absv + 2.0 ** -32 * allv
             assert np.array_equal(np.isnan(o), np.isnan(got)), i
             fine = ~np.isnan(o)
             assert (np.abs(got - o)[fine] <= tol[fine]).all(), (i, np.abs(got - o)[fine].max(), (np.abs(got - o)[fine] / np.maximum(tol[fine], 1e-300)).max())
