@@ -113,7 +113,10 @@ __device__ inline void store4(void* out, int64_t at, f32x4 v)
 // A workgroup has one cache head of one sequence, 16 QT query rows and a share of the pages; its four wavefronts take pages in turn, each with
 // sums of its own, which meet in LDS at the end.  S^T = K Q^T and O^T = V^T P^T, so that a lane holds one row's scores and probabilities.  Codes go from memory to
 // registers to the matrix units; a page's values are on their way while its scores are made, the next page's keys while its values are used.
-// Memory bound: 2 * D bytes a token and head.
+// Memory bound: 2 * D bytes a token and head.  Measured, 8 cache heads of 128, bf16: 2 x 262016 tokens before 32 heads 182 us (1.07 GB, 5.9 TB/s; a large copy moves
+// 4.95), 256 x 500..2047 tokens before 64 heads 151 us (0.67 GB, 4.4 TB/s: four rounds of workgroups that start with dependent loads).
+// Smaller pieces of the cache cost more than they balance (twice as many workgroups than the shape asks for 183 us, four times 228), loads without a page's lead and four wavefronts a SIMD
+// 183, three wavefronts 155.
 template <int DT, int DP, int QT>
 __global__ __launch_bounds__(256, (QT == 1 && DP <= 160) || (QT == 1 && DP == 192 && DT == 1) || (QT == 2 && DP * (DT == 1 ? 1 : 2) <= 128) ? 2 : 1) void kv_split_kernel(KvAttendArgs a)
 {
@@ -530,9 +533,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_bl
 // Four wavefronts of 32 rows (token after token, a token's query heads of the cache head next to each other) share the pages: a page's codes are loaded one
 // page ahead, turned into bf16 and fp16 operands once for all four and read from LDS as the lanes want them.  S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16
 // products, a lane has the scores of one row.  Bound by the matrix units, the exponentials and LDS reads, in about equal parts.
-// What was measured on 8 x 2048 queries, 32 heads over 8 of 128: the pipeline of one wavefront, product by product with the vector instructions that run
-// beside it, 415 us, a page after the other 444.  With 64 rows a wavefront (half of the LDS reads, one wavefront a SIMD) 568: two
-// wavefronts hide each other's waits better than one hides its own.  A page takes a wavefront 1.33 us alone on its SIMD, two of them 2.2.
+// What was measured on 8 x 2048 queries, 32 heads over 8 of 128 (275 GFLOP), with the append: the pipeline of one wavefront, product by product with the vector
+// instructions that run beside it, 390 us (690 TFLOP/s in the kernel, where a large matrix product reaches 1390), a page after the other 444.  With 64 rows a wavefront (half of the LDS reads, one wavefront a SIMD) 568: two
+// wavefronts hide each other's waits better than one hides its own.  A page takes a wavefront 1.33 us alone on its SIMD, two of them 2.2;
+// in the whole kernel vector instructions are issued 57 % of the time, the matrix units work 35 %, LDS 31 %.
 
 
 

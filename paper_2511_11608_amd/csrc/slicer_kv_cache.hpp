@@ -18,7 +18,7 @@ struct KvAppendArgs {
 // page of codes (amax over the 64 x D values of a head, scale = amax / 127, code = rint(x * (127 / amax)), three single fp32
 // operations), the last one that does not goes to the tail.  Where the first block reads the tail and the last one writes it, one workgroup makes
 // both; a head's other blocks are made of new tokens alone.  Memory bound: 2 bytes read and 1 written an element; all of a thread's loads
-// are under way before the first is used (one after the other: 37 us for 14 200 tokens of 8 x 128, bf16).
+// are under way before the first is used (14 200 tokens of 8 x 128, bf16, 87 MB: 21 us; one load after the other 37).
 // A token with a value that is not finite in its key or value is held as a NaN key and a zero value in the tail, and takes part in its page as
 // zeros under a NaN key scale: every query that sees the page (in the tail, the token) gets NaN, no other does.
 
@@ -207,7 +207,7 @@ struct KvReadArgs {
 };
 
 // What the cache stands for, a sequence's first tokens: code * scale in fp32 and the tail's bf16, rounded to the output's type once.
-// A record is read once, in its own order, and turned into rows through LDS; memory bound.
+// A record is read once, in its own order, and turned into rows through LDS; memory bound (14 200 tokens of 8 x 128, bf16, 87 MB: 17 us).
 template <int DT, int DP>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvReadArgs a)
 {
