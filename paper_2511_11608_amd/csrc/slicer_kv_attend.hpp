@@ -623,27 +623,30 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 31, h = lane >> 5;
     const int heads = a.kv.seqs * a.kv.G, D = a.kv.D;
     float2* const my_w = a.row_w + (size_t)blockIdx.x * a.slot_pages * TR;
-    for (int64_t tile = blockIdx.x; tile < (int64_t)heads * row_tiles * a.prompt_splits; tile += gridDim.x) {
+    // (fewer than 2^24 tiles, so that rows and tiles are numbers of 32 bits: divisions of 64 bits took a good part of a short tile's start)
+    const u32 R = (u32)a.R, n_tiles = (u32)heads * (u32)row_tiles * (u32)a.prompt_splits;
+    for (u32 tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
         // the longest tiles first; a head's tiles on one XCD (workgroup i runs on XCD i % 8), whose L2 its pages then are in
-        const int bg = (int)(tile % heads), split = (int)(tile / heads) % a.prompt_splits, rt = row_tiles - 1 - (int)(tile / heads) / a.prompt_splits;
-        const int b = bg / a.kv.G, g = bg % a.kv.G;
+        const u32 turn = tile / (u32)heads;
+        const int bg = (int)(tile - turn * (u32)heads), split = (int)(turn % (u32)a.prompt_splits), rt = row_tiles - 1 - (int)(turn / (u32)a.prompt_splits);
+        const int b = (int)((u32)bg / (u32)a.kv.G), g = bg - b * a.kv.G;
         KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
         const int n_all = s.n;
         s.n = s.n < a.max_new ? s.n : a.max_new;
-        const int64_t rows = (int64_t)s.n * a.R, row0 = (int64_t)rt * TR;
-        if (rows <= a.few_rows || row0 >= rows) continue;
-        const int64_t last_row = min(rows, row0 + TR) - 1;
-        const int most = a.causal ? max(0, s.len - n_all + (int)(last_row / a.R) + 1) : s.len;
-        const int least = a.causal ? s.len - n_all + (int)(row0 / a.R) + 1 : s.len;
+        const u32 rows = (u32)s.n * R, row0 = (u32)rt * TR;
+        if (rows <= (u32)a.few_rows || row0 >= rows) continue;
+        const u32 last_row = min(rows, row0 + TR) - 1;
+        const int most = a.causal ? max(0, s.len - n_all + (int)(last_row / R) + 1) : s.len;
+        const int least = a.causal ? s.len - n_all + (int)(row0 / R) + 1 : s.len;
         // this workgroup's share of the pages; from here on pages are counted from its first
         const KvShare share = kv_share((most + kPage - 1) / kPage, a.prompt_splits, split);
         const int full = s.len / kPage - share.first, units = share.end - share.first, ufull = max(min(units, full), 0);
         const int32_t* table = a.kv.table + (int64_t)b * a.kv.max_pages + share.first;
 
         bf16x8 q[NQ][KK];
-        const int64_t rr = row0 + wid * WR + c;
+        const u32 rr = row0 + wid * WR + c;
         const bool live = rr < rows;
-        const int qi = live ? (int)(rr / a.R) : 0, qh = g * a.R + (live ? (int)(rr % a.R) : 0);
+        const int qi = live ? (int)(rr / R) : 0, qh = g * a.R + (live ? (int)(rr - (u32)qi * R) : 0);
         const int lim = (!live ? 0 : a.causal ? s.len - n_all + qi + 1 : s.len) - share.first * kPage;
         const int64_t q_at = (s.first + qi) * a.q_token + qh * a.q_head + h * 8;
 #pragma unroll
