@@ -93,9 +93,10 @@ AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_n
     p.launch.row_blocks = p.splits > 1 ? p.rows_pad : 0;
     p.launch.page_blocks = p.rows_pad && mass && (p.splits > 1 || p.rows_pad > 16 || kv->max_pages > kMassPages) ? (int)((pages + 255) / 256) : 0;
     p.launch.prompt_tiles = rows > kSplitRows ? (int)((rows + kTileRows - 1) / kTileRows) : 0;
-    // Row tiles that do not fill the chip share their pages out, eight at least to a workgroup.
+    // Row tiles that do not fill the chip share their pages out, four at least to a workgroup (4 x 256..513 queries of 8 heads of 64 behind 3000 to 6000 tokens 103 -> 58 us a
+    // step; 1 x 1700 queries with no cache before them, where half of the tiles are short, 41 -> 46).
     const int64_t ptiles = pairs * std::max(p.launch.prompt_tiles, 1);
-    p.prompt_splits = ptiles < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / ptiles, pages / 8)) : 1;
+    p.prompt_splits = ptiles < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / ptiles, pages / 4)) : 1;
     p.launch.mass_blocks = mass && p.launch.prompt_tiles ? (int)((pages + (p.prompt_splits > 1 ? 3 : 255)) / (p.prompt_splits > 1 ? 4 : 256)) : 0;
     // Workgroups that have 1 KB a page each to keep a tile's weights in: all of them where pages are shared out; else at most 512, and 256 where 512 took
     // more than 2 GB.

@@ -450,7 +450,7 @@ __device__ inline float2 kv_row_total(const float2* ml, int splits, int lane)
 // A row's output from its parts, by a workgroup: all four wavefronts read parts at once, several a load (with one wavefront a row, part after part, 64 parts took
 // 64 us instead of 5).
 template <int DT, int DP>
-__device__ inline void kv_join_row(const KvAttendArgs& a, const float2* ml, const float* parts, int splits, float2 total, int64_t at, float bias, float (*xo)[DP])
+__device__ inline void kv_join_row(const KvAttendArgs& a, const float2* ml, const float* parts, int splits, float2 total, int64_t at, float (*xo)[DP])
 {
     constexpr int LPP = DP / 4, PPW = kWave / LPP;       // lanes a part, parts a load (one where a part takes more than half of the lanes)
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, D = a.kv.D;
@@ -482,7 +482,7 @@ __device__ inline void kv_join_row(const KvAttendArgs& a, const float2* ml, cons
         for (int w = 1; w < 4; ++w) v += *(const f32x4*)&xo[w][tid * 4];
         store4<DT>(a.out, at * D + tid * 4, v * (total.y == 0.0f ? 0.0f : 1.0f / total.y));
     }
-    if (tid == 0 && a.lse) a.lse[at] = total.y == 0.0f ? -__builtin_inff() : (total.x - bias + __log2f(total.y)) * kLn2;
+    if (tid == 0 && a.lse) a.lse[at] = total.y == 0.0f ? -__builtin_inff() : (total.x - kPBias + __log2f(total.y)) * kLn2;
 }
 
 // A row's share of a page's weight: its sum there under a maximum, the row's maximum and one over its sum.
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_bl
         if (blk >= rows) return;
         const int64_t slot = ((int64_t)bg * a.rows_pad + blk) * a.splits;
         const float2 ml = kv_row_total(a.part_ml + slot, a.splits, lane);
-        kv_join_row<DT, DP>(a, a.part_ml + slot, a.part_o + slot * DP, a.splits, ml, (s.first + blk / a.R) * a.H + g * a.R + blk % a.R, kPBias, xo);
+        kv_join_row<DT, DP>(a, a.part_ml + slot, a.part_o + slot * DP, a.splits, ml, (s.first + blk / a.R) * a.H + g * a.R + blk % a.R, xo);
         return;
     }
     for (int r = wid; r < rows; r += 4) {
@@ -1010,23 +1010,42 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
     }
 }
 
-// Rows of prompts whose pages were shared out (few row tiles before a long cache): a workgroup per row, as for the split rows.  With weights, the
-// rows' totals are kept for the pages' sums.
+// Rows of prompts whose pages were shared out (few row tiles before a long cache): a wavefront per row, several parts a load.  (A workgroup per row, as for the split
+// rows, whose parts are many: 35 us for 29000 rows of two parts.)  With weights, the rows' totals are kept for the pages' sums.
 template <int DT, int DP>
 __global__ __launch_bounds__(256) void kv_prompt_join_kernel(KvAttendArgs a, int row_tiles)
 {
-    __shared__ __align__(16) float xo[4][DP];
-    const int lane = threadIdx.x & 63;
-    const int64_t row = blockIdx.x, per_head = (int64_t)row_tiles * kTileRows;
-    const int bg = (int)(row / per_head), b = bg / a.kv.G, g = bg % a.kv.G;
-    const int64_t r = row % per_head;
+    constexpr int LPP = DP / 4, PPW = kWave / LPP;       // lanes a part, parts a load
+    const int lane = threadIdx.x & 63, D = a.kv.D, splits = a.prompt_splits;
+    const u32 row = blockIdx.x * 4 + (threadIdx.x >> 6), per_head = (u32)row_tiles * kTileRows;
+    const int bg = (int)(row / per_head), b = bg / a.kv.G, g = bg - b * a.kv.G;
+    const u32 r = row - (u32)bg * per_head;
     const KvSeq s = kv_seq(a.kv, a.starts, a.tokens, b);
-    const int64_t rows = (int64_t)min(s.n, a.max_new) * a.R;
-    if (rows <= a.few_rows || r >= rows) return;
-    const int64_t at = (s.first + r / a.R) * a.H + g * a.R + r % a.R;
-    const float2 ml = kv_row_total(a.prompt_ml + row * a.prompt_splits, a.prompt_splits, lane);
-    kv_join_row<DT, DP>(a, a.prompt_ml + row * a.prompt_splits, a.prompt_o + row * a.prompt_splits * DP, a.prompt_splits, ml, at, kPromptBias, xo);
-    if (threadIdx.x == 0 && a.mass) a.row_total[row] = float2{ml.x, 1.0f / ml.y};
+    const u32 rows = (u32)min(s.n, a.max_new) * (u32)a.R;
+    if (rows <= (u32)a.few_rows || r >= rows) return;
+    const u32 token = r / (u32)a.R;
+    const int64_t at = (s.first + token) * a.H + g * a.R + (r - token * (u32)a.R);
+    const float2* ml = a.prompt_ml + (size_t)row * splits;
+    const float* parts = a.prompt_o + (size_t)row * splits * DP;
+    const float2 total = kv_row_total(ml, splits, lane);
+    const int part = PPW > 1 ? lane / LPP : 0, d = (PPW > 1 ? lane % LPP : lane) * 4;
+    f32x4 v = {0, 0, 0, 0};
+    if (part < PPW && d < D) {
+#pragma unroll 4
+        for (int i = part; i < splits; i += PPW) v += *(const f32x4*)(parts + (size_t)i * DP + d) * exp2_of(ml[i].x - total.x);
+    }
+    if constexpr (PPW > 1) {
+#pragma unroll
+        for (int q = 1; q < PPW; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float f = __shfl(v[e], (lane + q * LPP) & 63);
+                if (part == 0) v[e] += f;
+            }
+    }
+    if (part == 0 && d < D) store4<DT>(a.out, at * D + d, v * (total.y == 0.0f ? 0.0f : 1.0f / total.y));
+    if (lane == 0 && a.lse) a.lse[at] = total.y == 0.0f ? -__builtin_inff() : (total.x - kPromptBias + __log2f(total.y)) * kLn2;
+    if (lane == 0 && a.mass) a.row_total[row] = float2{total.x, 1.0f / total.y};
 }
 
 // The pages' weights over the row tiles, in their order: of tiles that have summed their rows' up, or (pages shared out) over the rows, a wavefront a page.

@@ -83,7 +83,7 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, const KvAttendLaunch& p, hipS
             const unsigned tiles = pairs * (unsigned)(p.prompt_tiles * a.prompt_splits);
             hipLaunchKernelGGL((kv_prompt_kernel<DT, DP>), dim3(p.mass_blocks ? std::min(tiles, (unsigned)p.prompt_slots) : tiles), dim3(256), 0, st, a, p.prompt_tiles);
             if (a.prompt_splits > 1)
-                hipLaunchKernelGGL((kv_prompt_join_kernel<DT, DP>), dim3(pairs * (unsigned)(p.prompt_tiles * kTileRows)), dim3(256), 0, st, a, p.prompt_tiles);
+                hipLaunchKernelGGL((kv_prompt_join_kernel<DT, DP>), dim3(pairs * (unsigned)(p.prompt_tiles * kTileRows / 4)), dim3(256), 0, st, a, p.prompt_tiles);
             if (p.mass_blocks) hipLaunchKernelGGL((kv_mass_kernel<DT>), dim3(pairs * (unsigned)p.mass_blocks), dim3(256), 0, st, a, p.prompt_tiles, p.mass_blocks);
         }
     });
