@@ -87,9 +87,11 @@ AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_n
     p.rows_pad = even ? 0 : (int)std::min<int64_t>(rows, kSplitRows);
     p.launch.tile_rows = p.rows_pad > 16 && dp <= kWideTile ? 32 : 16;
     p.launch.split_tiles = (p.rows_pad + p.launch.tile_rows - 1) / p.launch.tile_rows;
-    // Four wavefronts of a workgroup take a page each; as many workgroups as the chip holds at once (two a CU), and no fewer than four pages each.
     const int64_t tiles = pairs * std::max(p.launch.split_tiles, 1);
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>((512 + tiles - 1) / tiles, (pages + 3) / 4));
+    // The cache is shared out while that gives no more than a workgroup a CU, and no further than a page for each of its four wavefronts.  Up to two a CU balance no better and
+    // leave more starts and more parts to join.  us for the append and the attention of a step, at most 256 workgroups and at least 512: 20 x 2000..2100 tokens, 8 heads of 256,
+    // fp32 74 and 105; 40 x 2000..2100, 8 of 160 70 and 81; 24 x 3000..5000, 8 of 64 29 and 32; 1 x 30000, 8 of 128 24 and 27; 2 x 262016 195 and 195.  At most 128: 2 x 262016 230.
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (pages + 3) / 4));
     p.launch.row_blocks = p.splits > 1 ? p.rows_pad : 0;
     p.launch.page_blocks = p.rows_pad && mass && (p.splits > 1 || p.rows_pad > 16 || kv->max_pages > kMassPages) ? (int)((pages + 255) / 256) : 0;
     p.launch.prompt_tiles = rows > kSplitRows ? (int)((rows + kTileRows - 1) / kTileRows) : 0;

@@ -115,8 +115,7 @@ __device__ inline void store4(void* out, int64_t at, f32x4 v)
 // registers to the matrix units; a page's values are on their way while its scores are made, the next page's keys while its values are used.
 // Memory bound: 2 * D bytes a token and head.  Measured, 8 cache heads of 128, bf16: 2 x 262016 tokens before 32 heads 182 us (1.07 GB, 5.9 TB/s; a large copy moves
 // 4.95), 256 x 500..2047 tokens before 64 heads 151 us (0.67 GB, 4.4 TB/s: four rounds of workgroups that start with dependent loads).
-// Smaller pieces of the cache cost more than they balance (twice as many workgroups than the shape asks for 183 us, four times 228), loads without a page's lead and four wavefronts a SIMD
-// 183, three wavefronts 155.
+// Of the second shape: loads without a page's lead and four wavefronts a SIMD 183 us, three wavefronts 155.
 template <int DT, int DP, int QT>
 __global__ __launch_bounds__(256, (QT == 1 && DP <= 160) || (QT == 1 && DP == 192 && DT == 1) || (QT == 2 && DP * (DT == 1 ? 1 : 2) <= 128) ? 2 : 1) void kv_split_kernel(KvAttendArgs a)
 {
