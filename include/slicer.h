@@ -315,7 +315,7 @@ int slicer_stream_words(const void* meta, uint64_t* words, void* hip_stream);
  * computations, are asynchronous on hip_stream, allocate nothing and can be captured into a HIP graph.  Calls that share a workspace, or of
  * which one writes what another reads, must be ordered by the caller; others may overlap.
  * Errors: SLICER_EINVAL for null pointers, seqs, heads, max_pages or n_pages < 1 (max_pages > 2^24, n_pages >= 2^31, seqs * kv_heads >= 2^22),
- * head_dim no multiple of 8 in 8..256, max_new < 1 with tokens > 0, tokens outside [0, 2^31), buffers off a 16-byte boundary, more than 2^24 workgroups,
+ * head_dim no multiple of 8 in 8..256, max_new < 1 with tokens > 0, tokens outside [0, 2^31), buffers off a 16-byte boundary, launches of 2^32 threads and more,
  * and what the calls name; SLICER_EUNSUPPORTED for an unknown dtype.
  */
 #define SLICER_KV_PAGE 64
@@ -376,7 +376,7 @@ int slicer_kv_read(const slicer_kv* kv, void* k, void* v, slicer_dtype dt, int64
  *   mass          [seqs][kv_heads][max_pages]
  *   page_table_out, lens_out, mass_out   as kv->page_table, kv->lens and mass, or those very arrays (no other overlap)
  *   freed         [seqs][max_pages]: the dropped pages in their order, then -1; n_freed [seqs]: how many
- *   workspace     12 * seqs * max_pages bytes, 256-byte aligned; contents undefined before and after
+ *   workspace     16 * seqs * max_pages bytes, 256-byte aligned; contents undefined before and after
  * pages, scales and tails of the handle are not looked at and may be NULL.
  * Errors: SLICER_EINVAL for negative counts or sink_pages + recent_pages > keep_pages.
  */

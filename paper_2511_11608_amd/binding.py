@@ -491,7 +491,7 @@ def alloc_kv_evict(kv: KvCache) -> KvEvicted:
     return KvEvicted(torch.empty_like(kv.page_table), torch.empty_like(kv.lens),
                      torch.empty(kv.seqs, kv.kv_heads, kv.max_pages, dtype=torch.float32, device=dev),
                      torch.empty_like(kv.page_table), torch.empty_like(kv.lens),
-                     torch.empty(12 * kv.seqs * kv.max_pages, dtype=torch.uint8, device=dev))
+                     torch.empty(16 * kv.seqs * kv.max_pages, dtype=torch.uint8, device=dev))
 
 
 def slicer_kv_evict(kv: KvCache, mass: torch.Tensor, keep_pages: int, sink_pages: int, recent_pages: int, out: KvEvicted, stream=None) -> None:
@@ -505,7 +505,7 @@ def slicer_kv_evict(kv: KvCache, mass: torch.Tensor, keep_pages: int, sink_pages
     _kv_tensor("out.mass", out.mass, torch.float32, by_head, dev)
     _kv_tensor("out.freed", out.freed, torch.int32, table, dev)
     _kv_tensor("out.n_freed", out.n_freed, torch.int32, (kv.seqs,), dev)
-    _kv_bytes("out.workspace", out.workspace, 12 * kv.seqs * kv.max_pages, dev)
+    _kv_bytes("out.workspace", out.workspace, 16 * kv.seqs * kv.max_pages, dev)
     _check("slicer_kv_evict", load().slicer_kv_evict(
         C.byref(c), mass.data_ptr(), keep_pages, sink_pages, recent_pages, out.page_table.data_ptr(), out.lens.data_ptr(), out.mass.data_ptr(),
         out.freed.data_ptr(), out.n_freed.data_ptr(), out.workspace.data_ptr(), _stream_handle(stream)))

@@ -256,7 +256,10 @@ int slicer_kv_evict(const slicer_kv* kv, const float* mass, int keep_pages, int 
     a.freed = freed;
     a.n_freed = n_freed;
     a.keys = (u64*)workspace;
-    a.from = (int32_t*)(a.keys + (size_t)kv->seqs * kv->max_pages);
+    a.chunks = (kv->max_pages + kEvictSmall - 1) / kEvictSmall;
+    a.cuts = (EvictCut*)(a.keys + (size_t)kv->seqs * kv->max_pages);
+    a.counts = (uint2*)(a.cuts + kv->seqs);
+    a.from = (int32_t*)(a.counts + (size_t)kv->seqs * a.chunks);
     hipStream_t st = (hipStream_t)hip_stream;
     const dim3 seqs((unsigned)kv->seqs);
     if (kv->max_pages <= 256) {
@@ -265,10 +268,11 @@ int slicer_kv_evict(const slicer_kv* kv, const float* mass, int keep_pages, int 
         hipLaunchKernelGGL(kv_evict_small_kernel<kEvictSmall>, seqs, dim3(kEvictSmall), 0, st, a);
     } else {
         const int64_t blocks = (kv->max_pages + 255) / 256;
-        if (blocks * kv->seqs >= kMaxGroups) return SLICER_EINVAL;
+        if (std::max<int64_t>(a.chunks, kv->kv_heads + 1) * kv->seqs >= kMaxGroups / 4) return SLICER_EINVAL;      // workgroups of 1024 threads; blocks <= 4 * chunks
         hipLaunchKernelGGL(kv_evict_keys_kernel, dim3((unsigned)(blocks * kv->seqs)), dim3(256), 0, st, a, (int)blocks);
-        hipLaunchKernelGGL(kv_evict_select_kernel, seqs, dim3(1024), 0, st, a);
-        hipLaunchKernelGGL(kv_evict_move_kernel, dim3((unsigned)(kv->seqs * kv->kv_heads)), dim3(1024), 0, st, a);
+        hipLaunchKernelGGL(kv_evict_cut_kernel, seqs, dim3(1024), 0, st, a);
+        hipLaunchKernelGGL(kv_evict_places_kernel, dim3((unsigned)(a.chunks * kv->seqs)), dim3(kEvictSmall), 0, st, a);
+        hipLaunchKernelGGL(kv_evict_move_kernel, dim3((unsigned)(kv->seqs * (kv->kv_heads + 1))), dim3(1024), 0, st, a);
     }
     return fail(hipGetLastError());
 }

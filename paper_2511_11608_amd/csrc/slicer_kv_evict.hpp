@@ -4,8 +4,9 @@
 // lower place.  A page's weight is the sum over the heads in fp64, in their order, so that its rank is that of the exact sum (fp32 sums would
 // rank near-equal pages by their rounding).  The last key that stays is found digit by digit from the highest bit in which keys differ; one ordered pass then
 // closes the gaps.  Source and destination may be the same arrays: whatever is written was read before, and nothing moves up.
-// Bound by latency: tables of up to 1024 pages take one launch, a page a thread; longer ones three, of which the first and the last, which touch the
-// weights, spread over the chip (1 x 16384 pages of 8 heads: 5 + 36 + 7 us; all in one workgroup 110).
+// Bound by latency: tables of up to 1024 pages take one launch, a page a thread; longer ones four, of which only the cut has one workgroup a sequence (1 x 16384 pages of 8
+// heads: keys 2.6, cut 19, places 5, moves 6.6 us).  The places in the cut's workgroup too: 40 us a call against 34, 1 x 40000 pages 93 against 71, but 256 x 1100 35 against
+// 37; in every head's move: 46; all in one workgroup 110.
 #pragma once
 
 #include "slicer_kv.hpp"
@@ -27,7 +28,10 @@ struct KvEvictArgs {
     int32_t* freed;
     int32_t* n_freed;
     u64* keys;                    // workspace, longer tables: [seqs][max_pages], then
-    int32_t* from;                // [seqs][max_pages] the place that a place's weight comes from, -1: none
+    struct EvictCut* cuts;        // [seqs]
+    uint2* counts;                // [seqs][chunks] keys above the cut and equal to it among kEvictSmall pages from `lo`
+    int32_t* from;                // [seqs][max_pages] the place that a place's entry comes from, -1: none
+    int chunks;
 };
 
 // Order-preserving key of a sum of weights; NaN above everything.
@@ -193,19 +197,18 @@ static __global__ __launch_bounds__(256) void kv_evict_keys_kernel(KvEvictArgs a
     if (r.need && p >= r.lo && p < r.hi) a.keys[(int64_t)b * a.max_pages + p] = evict_key(a, b, p);
 }
 
-// The table of one sequence, and where its weights come from, 16384 pages at a time.  Places come from ballots, 64 pages at a time (runs of 16 pages a
-// thread, whose loads and stores touch a line a lane: 46 us for 16384 pages).
-static __global__ __launch_bounds__(1024) void kv_evict_select_kernel(KvEvictArgs a)
+// The cut of one sequence, and how many keys are above and equal in each kEvictSmall pages of the range.
+static __global__ __launch_bounds__(1024) void kv_evict_cut_kernel(KvEvictArgs a)
 {
-    constexpr int BLOCK = 1024, E = kEvictRun;
+    constexpr int BLOCK = kEvictSmall, E = kEvictRun;
     __shared__ u32 hist[2048];
     __shared__ u64 ext[2 * BLOCK / kWave];
     __shared__ u32 scan[BLOCK / kWave + 1];
     __shared__ u32 sel[3];
-    const int b = blockIdx.x, tid = threadIdx.x, P = a.max_pages;
-    const int64_t row = (int64_t)b * P;
+    __shared__ u32 count[2 * E];
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const KvEvictRange r = evict_range(a, b);
-    const u64* keys = a.keys + row;
+    const u64* keys = a.keys + (int64_t)b * a.max_pages;
     EvictCut cut = {0, 0, 0};
     if (r.need) {
         // sixteen keys a thread; they stay in registers where that is all of them
@@ -224,90 +227,81 @@ static __global__ __launch_bounds__(1024) void kv_evict_select_kernel(KvEvictArg
                     if (base + e * BLOCK + tid < r.hi) use(k[e]);
             }
         }, hist, ext, scan, sel);
-    }
-    u32 gone_before = 0, equal_before = 0;
-    const int lane = tid & 63, wid = tid >> 6;
-    // prefix over the wavefronts of counts that are the same in all lanes of one
-    auto across = [&](u32 mine, u32* total) {
-        if (lane == 0) scan[wid] = mine;
-        __syncthreads();
-        u32 before = 0, sum = 0;
+        uint2* counts = a.counts + (int64_t)b * a.chunks;
+        for (int base = r.lo; base < r.hi; base += BLOCK * E) {
+            if (!once) load(base);
+            if (tid < 2 * E) count[tid] = 0;
+            __syncthreads();
 #pragma unroll
-        for (int w = 0; w < BLOCK / kWave; ++w) {
-            before += w < wid ? scan[w] : 0;
-            sum += scan[w];
-        }
-        __syncthreads();
-        *total = sum;
-        return before;
-    };
-    for (int base = 0; base < P; base += BLOCK * E) {
-        const int p0 = base + wid * (kWave * E) + lane;          // a wavefront has 1024 pages, 64 at a time
-        u64 key[E], equals[E], out[E];
-        int id[E];
-        u32 count = 0, n_equal, n_gone;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int p = p0 + e * kWave;
-            key[e] = r.need && p >= r.lo && p < r.hi ? keys[p] : 0;
-            id[e] = p < P ? a.table[row + p] : -1;
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int p = p0 + e * kWave;
-            equals[e] = __ballot(p >= r.lo && p < r.hi && (key[e] & cut.mask) == cut.prefix);
-            count += (u32)__popcll(equals[e]);
-        }
-        u32 at = across(count, &n_equal) + equal_before;
-        count = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int p = p0 + e * kWave;
-            out[e] = __ballot(p < P && p >= r.lo && p < r.hi && !evict_stays(cut, r.need, key[e], at + mask_rank(equals[e])));
-            at += (u32)__popcll(equals[e]);
-            count += (u32)__popcll(out[e]);
-        }
-        u32 before = across(count, &n_gone) + gone_before;       // (its barriers: everything here has been read)
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int p = p0 + e * kWave;
-            const u32 rank = before + mask_rank(out[e]);
-            before += (u32)__popcll(out[e]);
-            if (p >= P) continue;
-            if (out[e] >> lane & 1u) {
-                a.freed[row + rank] = id[e];
-            } else {
-                a.out_table[row + p - rank] = id[e];
-                a.from[row + p - rank] = p;
+            for (int e = 0; e < E; ++e) {
+                const bool in = base + e * BLOCK + tid < r.hi;
+                const u64 above = __ballot(in && (k[e] & cut.mask) > cut.prefix), equal = __ballot(in && (k[e] & cut.mask) == cut.prefix);
+                if (lane == 0 && above) atomicAdd(&count[2 * e], (u32)__popcll(above));
+                if (lane == 0 && equal) atomicAdd(&count[2 * e + 1], (u32)__popcll(equal));
             }
+            __syncthreads();
+            if (tid < E && base + tid * BLOCK < r.hi) counts[(base - r.lo) / BLOCK + tid] = make_uint2(count[2 * tid], count[2 * tid + 1]);
+            __syncthreads();
         }
-        equal_before += n_equal;
-        gone_before += n_gone;
     }
-    __syncthreads();
-    for (int p = tid; p < P; p += BLOCK) {
-        if (p >= P - (int)gone_before) {
-            a.out_table[row + p] = -1;
-            a.from[row + p] = -1;
-        }
-        if (p >= (int)gone_before) a.freed[row + p] = -1;
-    }
-    if (tid == 0) {
-        a.out_lens[b] = r.len - kPage * (int)gone_before;
-        a.n_freed[b] = (int)gone_before;
-    }
+    if (tid == 0) a.cuts[b] = cut;
 }
 
-// The weights of one sequence and head: 16384 places at a time are read before they are written.
+// Where a sequence's entries come from and which pages go, kEvictSmall pages of the range a workgroup, which counts what stays before them; the entries outside
+// the range are shared out.
+static __global__ __launch_bounds__(1024) void kv_evict_places_kernel(KvEvictArgs a)
+{
+    constexpr int BLOCK = kEvictSmall;
+    __shared__ u32 scan[BLOCK / kWave + 1];
+    const int b = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x, P = a.max_pages;
+    const int64_t row = (int64_t)b * P;
+    const KvEvictRange r = evict_range(a, b);
+    const EvictCut cut = a.cuts[b];
+    const int gone = r.hi - r.lo - (int)r.need;
+    const int first = r.lo + c * BLOCK, p = first + tid;
+    if (first < r.hi) {                                         // (the same for all threads)
+        u32 above = 0, equal = 0, n;
+        if (r.need) {
+            const uint2* counts = a.counts + (int64_t)b * a.chunks;
+            u32 mine = 0, equals = 0;
+            for (int i = tid; i < c; i += BLOCK) {
+                mine += counts[i].x;
+                equals += counts[i].y;
+            }
+            block_excl_scan<BLOCK>(mine, scan, &above);
+            block_excl_scan<BLOCK>(equals, scan, &equal);
+        }
+        const u32 before = above + (equal < cut.left ? equal : cut.left);       // that stay
+        const bool in = p < r.hi;
+        const u64 key = r.need && in ? a.keys[row + p] : 0;
+        const u32 equals = equal + block_excl_scan<BLOCK>(in && (key & cut.mask) == cut.prefix, scan, &n);
+        const bool stays = in && evict_stays(cut, r.need, key, equals);
+        const u32 rank = before + block_excl_scan<BLOCK>(stays, scan, &n);
+        if (stays) a.from[row + r.lo + rank] = p;
+        else if (in) a.freed[row + p - r.lo - rank] = a.table[row + p];
+    }
+    for (int q = c * BLOCK + tid; q < P; q += a.chunks * BLOCK) {
+        if (q < r.lo) a.from[row + q] = q;
+        else if (q >= r.hi) a.from[row + q - gone] = q;
+        if (q >= P - gone) a.from[row + q] = -1;
+        if (q >= gone) a.freed[row + q] = -1;
+    }
+    if (c == 0 && tid == 0) a.n_freed[b] = gone;
+}
+
+// Of one sequence the weights of a head, or the table: 16384 places at a time are read before they are written, since source and destination may be the same.
 static __global__ __launch_bounds__(1024) void kv_evict_move_kernel(KvEvictArgs a)
 {
     constexpr int BLOCK = 1024, E = kEvictRun;
-    const int b = blockIdx.x / a.G, P = a.max_pages;
-    const int32_t* from = a.from + (int64_t)b * P;
-    const float* mass = a.mass + (int64_t)blockIdx.x * P;
-    float* out = a.out_mass + (int64_t)blockIdx.x * P;
+    const int b = blockIdx.x / (a.G + 1), g = blockIdx.x % (a.G + 1), P = a.max_pages;
+    const int64_t row = (int64_t)b * P;
+    const bool table = g == a.G;
+    const int32_t* from = a.from + row;
+    const u32* in = table ? (const u32*)a.table + row : (const u32*)a.mass + row * a.G + (int64_t)g * P;
+    u32* out = table ? (u32*)a.out_table + row : (u32*)a.out_mass + row * a.G + (int64_t)g * P;
+    const u32 none = table ? (u32)-1 : 0;                       // the bits of -1 and of 0.0f
     for (int base = 0; base < P; base += BLOCK * E) {
-        float m[E];
+        u32 m[E];
         int at[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -315,7 +309,7 @@ static __global__ __launch_bounds__(1024) void kv_evict_move_kernel(KvEvictArgs 
             at[e] = p < P ? from[p] : -1;
         }
 #pragma unroll
-        for (int e = 0; e < E; ++e) m[e] = at[e] >= 0 ? mass[at[e]] : 0.0f;
+        for (int e = 0; e < E; ++e) m[e] = at[e] >= 0 ? in[at[e]] : none;
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -323,6 +317,10 @@ static __global__ __launch_bounds__(1024) void kv_evict_move_kernel(KvEvictArgs 
             if (p < P) out[p] = m[e];
         }
         __syncthreads();
+    }
+    if (table && threadIdx.x == 0) {
+        const KvEvictRange r = evict_range(a, b);
+        a.out_lens[b] = r.len - kPage * (r.hi - r.lo - (int)r.need);
     }
 }
 
