@@ -248,6 +248,24 @@ def test_long_cache_before_few_rows(past, new, heads, kv_heads, dim, dtype):
         p.check(new, q, dim ** -0.5, out, lse, causal, mass, old, 1.0)
 
 
+@pytest.mark.parametrize("seqs,heads,kv_heads,dim,new", [(33, 8, 4, 16, 1), (66, 8, 4, 24, 1), (43, 12, 3, 8, 5), (17, 16, 4, 16, 2), (130, 3, 1, 16, 1)])
+def test_steps_of_many_sequences_with_a_long_one(seqs, heads, kv_heads, dim, new):
+    """More row tiles than half of the chip, full and hardly full last rounds: shares of a long sequence, and ones that are empty in the others."""
+    torch = _torch()
+    past = [(37 * i) % 300 for i in range(seqs)]
+    past[seqs // 2], past[-1] = 6300, 6143
+    p = Pair(seqs, kv_heads, dim, 100, "bf16", seed=seqs)
+    p.append(past)
+    counts = [new if i % 5 else 0 for i in range(seqs)]
+    counts[seqs // 2] = counts[-1] = new
+    p.append(counts)
+    q = p.rand(sum(counts), heads)
+    mass = torch.rand(seqs, kv_heads, 100, device="cuda")
+    old = mass.clone()
+    out, lse = p.attend(counts, q.cuda(), dim ** -0.5, mass=mass, decay=0.5)
+    p.check(counts, q, dim ** -0.5, out, lse, mass=mass, old=old, decay=0.5)
+
+
 def test_many_tiles_give_the_same_bits_every_time():
     """Hundreds of workgroups whose wavefronts share operands in LDS: any order of theirs gives the same result."""
     torch = _torch()
