@@ -238,8 +238,8 @@ __global__ __launch_bounds__(256, (QT == 1 && DP <= 160) || (QT == 1 && DP == 19
             const bool there = id >= 0 && id < a.kv.n_pages;
             my_page = there ? id : 0;
             const float2 sc = *(const float2*)(a.kv.scales + (my_page * a.kv.G + g) * 2);
-            my_ks = there ? sc.x : __uint_as_float(0x7FC00000u);       // a page that is not there: NaN for who sees it
-            my_vs = sc.y;
+            my_ks = there ? sc.x : __uint_as_float(0x7FC00000u);       // a page that is not there: NaN for who sees it, zeros for the other rows
+            my_vs = there ? sc.y : 0.0f;
         }
     };
     auto record = [&](int i) {
@@ -700,7 +700,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                 my_page = there ? (u32)id : 0u;
                 const float2 sc = *(const float2*)(a.kv.scales + ((int64_t)my_page * a.kv.G + g) * 2);
                 my_ks = there ? sc.x : __uint_as_float(0x7FC00000u);
-                my_vs = sc.y;
+                my_vs = there ? sc.y : 0.0f;
             }
         };
         auto load_keys = [&](int lane_of) {
