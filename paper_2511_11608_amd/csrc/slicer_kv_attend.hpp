@@ -205,12 +205,14 @@ __global__ __launch_bounds__(256, (QT == 1 && DP <= 160) || (QT == 1 && DP == 19
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         const float mn = fmaxf(m[x], mx), ms = mn == -__builtin_inff() ? 0.0f : mn;
-        const float alpha = exp2_of(m[x] - ms), off = kPBias - ms;
+        const float alpha = exp2_of(m[x] - ms);
         float sum = 0.0f;
+        // (the maximum first: under it every difference is right to half a step of its own, whereas bias - maximum is rounded to the maximum's, from 2^26 on
+        // to more than fp16's room above 2^13)
 #pragma unroll
         for (int T = 0; T < 4; ++T)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) { sc[T][r] = exp2_of(sc[T][r] + off); sum += sc[T][r]; }
+            for (int r = 0; r < 4; ++r) { sc[T][r] = exp2_of((sc[T][r] - ms) + kPBias); sum += sc[T][r]; }
         m[x] = mn;
         l[x] = __builtin_fmaf(l[x], alpha, sum);
         if (a.mass) {

@@ -1,7 +1,14 @@
-"""The attention cache in 8 bits at the ends of its range."""
+"""The attention cache in 8 bits at the ends of its range: pages that are not there, scores and values far from one, lengths that are taken back.
+
+Scores here are exact: keys are whole numbers (a page's largest magnitude is 127, its scale 1) and a query is a power of two in one element, so that equal
+scores are equal in 32 bits too and others are so far apart that their weights are 0.  What is left of a tolerance is half a step of the output's
+type, the probabilities' rounding (fp16 2^-11; two fp16 numbers 2^-21) and fp32 sums over the tokens, length * 2^-24, the last two times sum p |v|: a weight of
+0 allows nothing, however large its value.
+"""
 import numpy as np
 import pytest
 
+from tests.kv_ref import PAGE
 from tests.test_gpu_kv import Pair, starts_of
 
 pytestmark = pytest.mark.gpu
@@ -10,6 +17,36 @@ pytestmark = pytest.mark.gpu
 def _torch():
     import torch
     return torch
+
+
+def check_exact_scores(p, counts, q, scale, out, lse, mass=None):
+    torch = _torch()
+    fi, at = torch.finfo(q.dtype), 0
+    p_bits = 2.0 ** -11 if q.dtype == torch.bfloat16 else 2.0 ** -21
+    for i, (r, n) in enumerate(zip(p.ref, counts)):
+        o, l, w, absv, _, _ = r.attend(q[at: at + n], scale)
+        got, got_l = out[at: at + n].double().cpu().numpy(), lse[at: at + n].double().cpu().numpy()
+        at += n
+        tol = fi.eps / 2 * (1 + 2.0 ** -7) * np.abs(o) + fi.eps / 2 * fi.smallest_normal + (p_bits + (len(r) + 64) * 2.0 ** -24) * absv
+        assert np.array_equal(np.isnan(o), np.isnan(got)), (i, np.argwhere(np.isnan(o) != np.isnan(got))[:4])
+        wrong = ~np.isnan(o) & ~(np.abs(got - o) <= tol)
+        assert not wrong.any(), (i, np.argwhere(wrong)[:4], got[wrong][:4], o[wrong][:4])
+        # scale times log2(e), its product with a score, and the way back: six roundings of 2^-24
+        assert np.array_equal(np.isnan(l), np.isnan(got_l)), i
+        fine = ~np.isnan(l)
+        assert (np.abs(got_l - l)[fine] <= 6 * 2.0 ** -24 * np.abs(l)[fine] + 2.0 ** -20).all(), (i, np.abs(got_l - l)[fine].max())
+        if mass is not None and n:
+            g = mass[i].double().cpu().numpy()[:, : w.shape[1]]
+            assert (np.abs(g - w) <= ((len(r) + n * q.shape[1] + 64) * 2.0 ** -24 + 2.0 ** -21) * w + 2.0 ** -126).all(), (i, g, w)      # (a weight below fp32's range is 0)
+
+
+def whole_keys(codes, dim, dtype):
+    """Keys whose element 0 is the token's code and whose element 1 is 127."""
+    torch = _torch()
+    k = torch.zeros(len(codes), 1, dim)
+    k[:, 0, 0] = torch.as_tensor(codes, dtype=torch.float32)
+    k[:, 0, 1] = 127.0
+    return k.to(dtype)
 
 
 @pytest.mark.parametrize("fill", [float("inf"), 3e38, float("nan"), 0.0])
@@ -37,3 +74,34 @@ def test_a_page_that_is_not_there_reaches_only_who_sees_it(n, max_new, fill):
         assert not seen[0].any() and seen[1:max_new].all()  # the first query's own token is the last one before the page
         p.check([n], q, 0.125, torch.cat([out[:max_new].cpu(), torch.full((n - max_new, 1, 64), float("nan"), dtype=p.dt)]),
                 torch.cat([lse[:max_new].cpu(), torch.full((n - max_new, 1), float("nan"))]))
+
+
+ROWS = [(1, 400), (4, 400), (16, 700), (70, 400), (130, 0), (300, 900)]        # new tokens before 2 heads, tokens before them
+
+
+def large_scores(rows, exponent, dtype, rising):
+    torch = _torch()
+    n, past = rows
+    p = Pair(1, 1, 40, -(-(n + past) // PAGE), dtype, seed=n + exponent)
+    rng = np.random.default_rng(exponent + n)
+    total = n + past
+    # a narrow range of codes that moves on with the tokens: the maximum changes from page to page
+    codes = np.linspace(-100, 100, total).astype(int) * (1 if rising else -1) + rng.integers(-20, 21, total)
+    k, v = whole_keys(codes, 40, p.dt), p.rand(total, 1)
+    if past:
+        p.append([past], k[:past], v[:past])
+    p.append([n], k[past:], v[past:])
+    q = torch.zeros(n, 2, 40)
+    q[:, 0, 0], q[:, 1, 0] = 2.0 ** exponent, -2.0 ** exponent
+    q = q.to(p.dt)
+    mass = torch.zeros(1, 1, p.kv.max_pages, device="cuda")
+    out, lse = p.attend([n], q.cuda(), 0.125, mass=mass)
+    check_exact_scores(p, [n], q, 0.125, out, lse, mass)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("exponent", [14, 20, 23, 24, 26, 30, 60, 100])
+@pytest.mark.parametrize("rows", [r for r in ROWS if r[0] <= 32])
+def test_large_scores_of_split_rows(rows, exponent, dtype):
+    for rising in (True, False):
+        large_scores(rows, exponent, dtype, rising)
