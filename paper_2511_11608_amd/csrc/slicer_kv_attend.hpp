@@ -604,6 +604,9 @@ __device__ inline void stage_tail(uint16_t* keys, uint16_t* values, const uint16
 // Probabilities are held times 2^8 here: a row's maximum may grow by 2^6 before its sums are scaled down to it (nearly every page raises the
 // maximum of some row, hardly any by that much), and a page's value scale may be twice the one that outputs are held in: 2^15 at most in fp16.
 constexpr float kPromptBias = 8.0f, kSlack = 6.0f;
+// Maxima beyond this (times log2(e); no model's) are not for the pipeline: its exponent, score * factor + (bias - maximum) in one instruction, takes a product that was
+// not rounded from a maximum that was, and is off by half a step of it: 2^-13 here, as much as the score itself, but more than fp16's room from 2^24 on.
+constexpr float kSteep = 4096.0f;
 
 __device__ inline float other_half(float x, float* mine)             // the values of lanes l and l + 32 of a pair, in both of them
 {
@@ -621,6 +624,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
     constexpr int WR = 32, TR = kTileRows;               // rows of a wavefront, of the tile
     __shared__ __align__(16) uint16_t buf[2][PromptTile<DP>::kAll];
     __shared__ float2 xrow[TR];
+    __shared__ int xcareful;
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, c = lane & 31, h = lane >> 5;
     const int heads = a.kv.seqs * a.kv.G, D = a.kv.D;
     float2* const my_w = a.row_w + (size_t)blockIdx.x * a.slot_pages * TR;
@@ -661,6 +665,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
 
         // outputs are held in units of vref, the scale of some page; the same in all wavefronts
         float m = -__builtin_inff(), l = 0.0f, vref = 0.0f, vmax = 0.0f;
+        bool careful = false;                            // the pages have to be gone through again, see below
         f32x16 o[DL];
 #pragma unroll
         for (int t = 0; t < DL; ++t)
@@ -755,6 +760,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                 rescale(alpha);
                 l *= alpha;
                 m = mn;
+                careful |= fabsf(m) > kSteep && m != -__builtin_inff();
             }
         };
         auto page_weight = [&](int u, float sum) {
@@ -801,7 +807,34 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
             }
         };
 
+        // outside the pipeline: scores -> probabilities times 2^8 under their exact maximum; returns what the sums so far are to be multiplied by
+        auto weigh = [&](f32x16* sc, int u) {
+            const int left = lim - u * kPage - h * 4;
+            float mx = -__builtin_inff(), here, sum = 0.0f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    sc[t][r] = t * 32 + (r >> 2) * 8 + (r & 3) < left ? sc[t][r] * factor : -__builtin_inff();
+                    mx = fmaxf(mx, sc[t][r]);
+                }
+            mx = other_half(mx, &here);
+            const float mn = fmaxf(m, fmaxf(mx, here)), ms = mn == -__builtin_inff() ? 0.0f : mn, alpha = exp2_of(m - ms);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    sc[t][r] = exp2_of((sc[t][r] - ms) + kPromptBias);
+                    sum += sc[t][r];
+                }
+            m = mn;
+            l = __builtin_fmaf(l, alpha, sum);
+            page_weight(u, sum);
+            return alpha;
+        };
+
         __syncthreads();                                 // (the tile before may still be read)
+        if (tid == 0) xcareful = 0;
         // The pages in a pipeline: while a page's probabilities are made and multiplied by its values, the next page's scores are
         // made, and the operands of the keys behind those and of the next values go to LDS: matrix and vector instructions of one wavefront
         // run at the same time.  Page u has its keys in buf[u % 2] one step before its values.
@@ -923,6 +956,53 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
             l = __builtin_fmaf(sum, back, l);
             page_weight(u, sum);
             products(buf[u & 1] + PromptTile<DP>::kKeys, sa);
+            if (careful) xcareful = 1;
+            __syncthreads();
+            if (xcareful) {
+                // what the pipeline cannot hold: page after page, the products of each on their own, outputs in units of 1
+                vref = back = 1.0f;
+                m = -__builtin_inff();
+                l = 0.0f;
+#pragma unroll
+                for (int t = 0; t < DL; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[t][r] = 0.0f;
+                for (u = 0; u < ufull; ++u) {
+                    if ((u & 63) == 0) fetch(u);
+                    load_keys(u & 63);
+                    load_values(u & 63);
+                    __syncthreads();
+                    stage_k(0);
+                    stage_v(0);
+                    __syncthreads();
+                    factor = __uint_as_float(bcast(__float_as_uint(my_ks), u & 63)) * a.scale;
+                    const float vs = __uint_as_float(bcast(__float_as_uint(my_vs), u & 63));
+                    scores(buf[0], sa);
+                    const float alpha = weigh(sa, u);
+                    f16x8 p[4][NP];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float f = sa[e >> 4][e & 15];
+                        const _Float16 hi = (_Float16)f;
+                        p[e >> 3][0][e & 7] = hi;
+                        if constexpr (NP > 1) p[e >> 3][1][e & 7] = (_Float16)(f - (float)hi);
+                    }
+#pragma unroll
+                    for (int t = 0; t < DL; ++t) {
+                        f32x16 acc;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const f16x8 v = *(const f16x8*)(buf[0] + PromptTile<DP>::kKeys + ((t * 4 + k) * 64 + lane) * 8);
+#pragma unroll
+                            for (int i = 0; i < NP; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k][i], acc, 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) o[t][r] = __builtin_fmaf(acc[r], vs, o[t][r] * alpha);
+                    }
+                }
+            }
         }
         if (units > max(full, 0)) {                      // the tail is in this share
             const int count = s.len % kPage;
@@ -931,19 +1011,11 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
             __syncthreads();
             f32x16 sc[2];
             scores(buf[0], sc);
-            rescale(vref);
-            vref = 1.0f;
             factor = a.scale;
-            lr = 0.0f;
             back = 1.0f;
             const uint16_t* values = buf[0] + PromptTile<DP>::kKeys;
-            new_maximum(lane_max(std::true_type(), sc, full));
-            const float off = kPromptBias - finite_max();
-            float sum = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) sum += exponential(std::true_type(), sc, e, lim - full * kPage - h * 4, off);
-            l += sum;
-            page_weight(full, sum);
+            rescale(weigh(sc, full) * vref);
+            vref = 1.0f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 bf16x8 p[NB];

@@ -105,3 +105,11 @@ def large_scores(rows, exponent, dtype, rising):
 def test_large_scores_of_split_rows(rows, exponent, dtype):
     for rising in (True, False):
         large_scores(rows, exponent, dtype, rising)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("exponent", [14, 20, 23, 24, 26, 30, 60, 100])
+@pytest.mark.parametrize("rows", [r for r in ROWS if r[0] > 32])
+def test_large_scores_of_prompts(rows, exponent, dtype):
+    for rising in (True, False):
+        large_scores(rows, exponent, dtype, rising)
