@@ -664,7 +664,7 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
         }
 
         // outputs are held in units of vref, the scale of some page; the same in all wavefronts
-        float m = -__builtin_inff(), l = 0.0f, vref = 0.0f, vmax = 0.0f;
+        float m = -__builtin_inff(), l = 0.0f, vref = 0.0f, vfirst = 0.0f;
         bool careful = false;                            // the pages have to be gone through again, see below
         f32x16 o[DL];
 #pragma unroll
@@ -733,20 +733,22 @@ __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv
                 if (mine(i >> 2)) stage_values<DP>(buf[which] + PromptTile<DP>::kKeys, (i >> 2) * 256 + tid, vb[i >> 2], i & 3);
         };
         // what a page's scores are multiplied by, and its value scale over vref: its logarithm and inverse.  vref follows the scales: a page's is within
-        // 2^-6 .. 2 of it, so that probabilities keep their bits; less than 2^-60 of the largest counts as that (a page of zeros: any)
+        // 2^-6 .. 2 of it, so that probabilities keep their bits (a page of zeros: any).  Scales more than 2^30 from the first are not for the pipeline: a row's sums
+        // in units of a page that it has no weight on would leave fp32's range
         float factor = 0.0f, lr = 0.0f, back = 1.0f;
         auto page_scales = [&](int lane_of) {
             const float ks = __uint_as_float(bcast(__float_as_uint(my_ks), lane_of)), vs = __uint_as_float(bcast(__float_as_uint(my_vs), lane_of));
             factor = ks * a.scale;
-            vmax = fmaxf(vmax, vs);
-            const float vt = fmaxf(vs, vmax * 0x1p-60f);
-            if (vt > 2.0f * vref || (vs > 0.0f && vt < vref * 0.015625f)) {
+            if (vs > 2.0f * vref || (vs > 0.0f && vs < vref * 0.015625f)) {
                 if (vref > 0.0f) {
-                    rescale(vref / vt);
+                    rescale(vref / vs);
+                    careful |= vs > vfirst * 0x1p30f || vs < vfirst * 0x1p-30f;
+                } else {
+                    vfirst = vs;
                 }
-                vref = vt;
+                vref = vs;
             }
-            const float ratio = vs > 0.0f ? vt * __builtin_amdgcn_rcpf(vref) : 1.0f;
+            const float ratio = vs > 0.0f ? vs * __builtin_amdgcn_rcpf(vref) : 1.0f;
             lr = __log2f(ratio);
             back = __builtin_amdgcn_rcpf(ratio);
         };

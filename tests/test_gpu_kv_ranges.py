@@ -113,3 +113,32 @@ def test_large_scores_of_split_rows(rows, exponent, dtype):
 def test_large_scores_of_prompts(rows, exponent, dtype):
     for rising in (True, False):
         large_scores(rows, exponent, dtype, rising)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [3, 100, 200])
+@pytest.mark.parametrize("order", ["LSTZ", "SLTZ", "STLZ", "TSZL", "ZTLS", "LTEZ", "TLZE"])
+def test_values_of_any_scale(order, n, dtype):
+    """Pages whose values are far apart: L large (2^90) under a score between the others', S (2^-7) and T (2^-95) under the scores that queries look for,
+    Z zeros, E as large as L with S's score, zeros in one element: every row is made of the pages that it has weight on, in every element."""
+    torch = _torch()
+    p = Pair(1, 1, 32, 4 + -(-n // PAGE), dtype, seed=n)
+    codes = {"L": 0, "S": 50, "T": -50, "Z": 3, "E": 50}
+    size = {"L": 2.0 ** 90, "S": 2.0 ** -7, "T": 2.0 ** -95, "Z": 0.0, "E": 2.0 ** 90}
+    k = whole_keys(np.concatenate([np.full(PAGE, codes[c]) for c in order] + [np.zeros(n)]), 32, p.dt)
+    v = p.rand(4 * PAGE + n, 1).float().clamp(-4.0, 4.0)
+    for i, c in enumerate(order):
+        v[i * PAGE: i * PAGE + PAGE] *= size[c]
+        if c == "E":
+            v[i * PAGE: i * PAGE + PAGE, 0, 5] = 0.0
+    if "E" in order:                                        # (its partner is S's place in the tokens that follow)
+        k[4 * PAGE:, 0, 0] = 50.0
+    v = v.to(p.dt)
+    p.append([4 * PAGE], k[: 4 * PAGE], v[: 4 * PAGE])
+    p.append([n], k[4 * PAGE:], v[4 * PAGE:])
+    q = torch.zeros(n, 2, 32)
+    q[:, 0, 0], q[:, 1, 0] = 32.0, -32.0                   # 200 between L and what is looked for
+    q = q.to(p.dt)
+    mass = torch.zeros(1, 1, p.kv.max_pages, device="cuda")
+    out, lse = p.attend([n], q.cuda(), 0.125, mass=mass)
+    check_exact_scores(p, [n], q, 0.125, out, lse, mass)
