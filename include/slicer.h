@@ -302,8 +302,11 @@ int slicer_stream_words(const void* meta, uint64_t* words, void* hip_stream);
  *            that is not full yet are held so, in the sequence's tail.  When a page gets full its 64 x head_dim keys of a head are held as
  *            code * scale, with amax their largest magnitude: scale = amax / 127, code = rint(x * (127 / amax)) within -127..127, every step one fp32
  *            operation; values likewise, with a scale of their own.  amax < 2^-119: zeros.  The result does not depend on how many tokens a call brings.
- *   values   queries, keys and values finite, magnitudes up to 2^100.  A token with others is held as a key of NaN and a value of zero, in a full page as zeros under a key scale of
- *            NaN: outputs of queries that see it (in a full page: that see the page) are NaN, no others are touched.
+ *   values   queries, keys and values finite, magnitudes up to 2^100, a value's times the sequence's tokens up to 2^112.  Scores are fp32: for a query and a key the sum of |q k| over
+ *            their elements, scale times that, and scale times any element of the key stay below 2^126.  Within that a score may be of any size; it is as right as an fp32
+ *            sum is, 2^-24 of the sum of |q k| a step, and a weight below 2^-27 of the row's largest may count as zero.  A token with other keys or values is held as a key of
+ *            NaN and a value of zero, in a full page as zeros under a key scale of NaN: outputs of queries that see it (in a full page: that see the page) are NaN, no others
+ *            are touched.
  *   handle   slicer_kv is read on the host during a call; its pointers are device memory of the caller, 256-byte aligned, sizes from slicer_kv_sizes.
  *            pages, scales and tails need no initial values.  page_table and lens are the caller's to keep, on the device; entries that
  *            lie outside the cache are never followed: a page_table entry outside [0, n_pages) is not written, and read as NaN; lens are taken as
@@ -355,7 +358,7 @@ int slicer_kv_append(const slicer_kv* kv, const void* k, const void* v, slicer_d
  *   workspace  slicer_kv_attend_sizes bytes (with_mass: for calls with mass; enough for those without), 256-byte aligned; contents undefined before and after
  *   max_len    what lens are expected to stay within; it decides how the work is split, never the result's validity
  * The result is a function of the arguments alone: nothing is summed in an order that changes from call to call.
- * Errors: SLICER_EINVAL for heads no multiple of kv_heads, scale not finite, mass_decay outside [0, 1], max_len < 0.
+ * Errors: SLICER_EINVAL for heads no multiple of kv_heads, scale (times log2(e)) not finite in fp32, mass_decay outside [0, 1], max_len < 0.
  */
 int slicer_kv_attend_sizes(const slicer_kv* kv, int heads, int64_t tokens, int max_new, int64_t max_len, int with_mass, size_t* workspace_bytes);
 int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int heads, int64_t tokens, const int32_t* starts, int max_new,

@@ -178,7 +178,8 @@ int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int he
 {
     int rc = check_call(kv, (int)dt, tokens, starts, max_new);
     if (rc) return rc;
-    if (heads < 1 || heads % kv->kv_heads || !std::isfinite(scale) || !(mass_decay >= 0.0 && mass_decay <= 1.0) || max_len < 0) return SLICER_EINVAL;
+    const float scale2 = (float)(std::fabs(scale) * 1.44269504088896340736);           // of scores that are exponents of 2
+    if (heads < 1 || heads % kv->kv_heads || !std::isfinite(scale2) || !(mass_decay >= 0.0 && mass_decay <= 1.0) || max_len < 0) return SLICER_EINVAL;
     if (tokens == 0) return SLICER_OK;
     if (!q || !out || !workspace || (((uintptr_t)out | (uintptr_t)workspace) & 15)) return SLICER_EINVAL;
     const AttendPlan p = plan_attend(kv, heads, tokens, max_new, max_len, mass != nullptr);
@@ -196,7 +197,7 @@ int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int he
     a.H = heads;
     a.max_new = max_new;
     a.causal = causal != 0;
-    a.scale = (float)(std::fabs(scale) * 1.44269504088896340736);
+    a.scale = scale2;
     a.flip = scale < 0.0;
     a.out = out;
     a.lse = lse;

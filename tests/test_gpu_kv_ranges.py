@@ -142,3 +142,26 @@ def test_values_of_any_scale(order, n, dtype):
     mass = torch.zeros(1, 1, p.kv.max_pages, device="cuda")
     out, lse = p.attend([n], q.cuda(), 0.125, mass=mass)
     check_exact_scores(p, [n], q, 0.125, out, lse, mass)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 70])
+@pytest.mark.parametrize("max_len", [0, 70000])
+def test_the_largest_values_of_a_long_cache(max_len, n, dtype):
+    """Sums of 70000 values of 2^95, before they are divided by the weights' sum: a value times the tokens is below 2^112; the first page's scores are 4 below the others', too little for a new maximum
+    of a prompt's rows."""
+    torch = _torch()
+    p = Pair(1, 1, 8, -(-70000 // PAGE), dtype, seed=n)
+    v = torch.full((70000, 1, 8), 2.0 ** 95).to(p.dt)
+    k, q = torch.zeros(70000, 1, 8), torch.zeros(n, 2, 8)
+    k[PAGE:, 0, 0], q[:, :, 0] = 16.0, 1.0
+    k, q = k.to(p.dt), q.to(p.dt)
+    for first, count in ((0, 70000 - n), (70000 - n, n)):
+        p.kv.lens.fill_(first + count)
+        p.b.slicer_kv_append(p.kv, k[first: first + count].cuda(), v[first: first + count].cuda(), starts_of([count]), count)
+    p.ref[0].open = [None] * 70000                          # (only their number)
+    for causal in (True, False):
+        out, _ = p.attend([n], q.cuda(), 0.25, causal, max_len=max_len)
+        # half a step, the probabilities' rounding, and sums in fp32, of the values and of the weights
+        off = torch.finfo(p.dt).eps / 2 + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -21) + 2 * 70064 * 2.0 ** -24
+        assert (np.abs(out.double().cpu().numpy() / 2.0 ** 95 - 1.0) <= off).all()
