@@ -360,30 +360,33 @@ class KvCache:
     def __init__(self, pages, scales, tails, page_table, lens, seqs, kv_heads, head_dim, n_pages, max_pages):
         self.pages, self.scales, self.tails, self.page_table, self.lens = pages, scales, tails, page_table, lens
         self.seqs, self.kv_heads, self.head_dim, self.n_pages, self.max_pages = seqs, kv_heads, head_dim, n_pages, max_pages
-        self._c, self._key, self._held, self._need = None, None, (), (None, 0)
+        # what was checked and computed last, each replaced as a whole: calls of other threads on the same cache may put theirs there at any time
+        self._checked, self._need = (None, (), None), (None, None, 0)
 
     def c(self) -> SlicerKv:
         """The C handle of the tensors as they are now; they are checked when one of them or a size is another than before."""
         t = (self.pages, self.scales, self.tails, self.page_table, self.lens)
         key = (self.pages.data_ptr(), self.scales.data_ptr(), self.tails.data_ptr(), self.page_table.data_ptr(), self.lens.data_ptr(),
                self.seqs, self.kv_heads, self.head_dim, self.max_pages, self.n_pages)
-        if key != self._key or any(a is not b for a, b in zip(t, self._held)):
+        known = self._checked
+        if key != known[0] or any(a is not b for a, b in zip(t, known[1])):
             dev = self.pages.get_device()
             _kv_tensor("page_table", self.page_table, torch.int32, (self.seqs, self.max_pages), dev)
             _kv_tensor("lens", self.lens, torch.int32, (self.seqs,), dev)
             sizes = _kv_sizes(SlicerKv(None, None, None, None, None, *key[5:]))
             for name, x, size in zip(("pages", "scales", "tails"), t, sizes):
                 _kv_bytes(name, x, size, dev)
-            self._c, self._key, self._held, self._need = SlicerKv(*key), key, t, (None, 0)
-        return self._c
+            known = self._checked = (key, t, SlicerKv(*key))
+        return known[2]
 
     def workspace_bytes(self, c, *shape) -> int:
         """slicer_kv_attend_sizes for heads, tokens, max_new, max_len, with_mass."""
-        if self._need[0] != shape:
+        known = self._need
+        if known[0] is not c or known[1] != shape:
             w = C.c_size_t(0)
             _check("slicer_kv_attend_sizes", load().slicer_kv_attend_sizes(C.byref(c), *shape, C.byref(w)))
-            self._need = (shape, w.value)
-        return self._need[1]
+            known = self._need = (c, shape, w.value)
+        return known[2]
 
 
 class KvEvicted:

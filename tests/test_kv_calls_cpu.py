@@ -1,4 +1,4 @@
-"""slicer_kv_*, calls that need no GPU: refusals of scales that fp32 does not hold."""
+"""slicer_kv_*, calls that need no GPU: refusals of scales that fp32 does not hold, workspace sizes of calls made at the same time."""
 import pytest
 
 from tests.test_kv_cpu import attend, handle, lib  # noqa: F401 (a fixture)
@@ -8,3 +8,36 @@ from tests.test_kv_cpu import attend, handle, lib  # noqa: F401 (a fixture)
 def test_scales_beyond_fp32_are_refused(lib, scale):  # noqa: F811
     """3e38 is finite in fp32, and times log2(e) it is not."""
     assert attend(lib, handle(), scale=scale) == -1
+
+
+class Turn(int):
+    """A number that hands the turn to another thread's call while it is compared."""
+    other = None
+
+    def __eq__(self, x):
+        if Turn.other:
+            call, Turn.other = Turn.other, None
+            call()
+        return int(self) == int(x)
+
+    def __ne__(self, x):
+        return not self == x
+
+    __hash__ = int.__hash__
+
+
+def test_workspace_sizes_of_two_calls_at_once(lib):  # noqa: F811
+    """The size that a call checks its workspace against is that of its own shape, whatever another call on the same cache does between its steps."""
+    from paper_2511_11608_amd import binding
+    kv, c = binding.alloc_kv(2, 4, 64, 16, 8, device="cpu"), handle()
+    small, large = (8, 2, 1, 100, 0), (8, 4000, 2000, 512, 1)
+    want = [binding.KvCache.workspace_bytes(binding.alloc_kv(2, 4, 64, 16, 8, device="cpu"), c, *shape) for shape in (small, large)]
+    assert 0 < want[0] < want[1]
+    for mine, others, size in ((large, small, want[1]), (small, large, want[0])):
+        shape = tuple(Turn(x) for x in mine)
+        assert kv.workspace_bytes(c, *shape) == size
+        Turn.other = lambda: kv.workspace_bytes(c, *others)
+        assert kv.workspace_bytes(c, *(Turn(x) for x in mine)) == size
+        assert Turn.other is None
+    # and of another handle of the same cache
+    assert kv.workspace_bytes(handle(seqs=200), *large) > want[1] and kv.workspace_bytes(c, *large) == want[1]
