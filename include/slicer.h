@@ -311,6 +311,10 @@ int slicer_stream_words(const void* meta, uint64_t* words, void* hip_stream);
  *            pages, scales and tails need no initial values.  page_table and lens are the caller's to keep, on the device; entries that
  *            lie outside the cache are never followed: a page_table entry outside [0, n_pages) is not written, and read as NaN; lens are taken as
  *            if within [0, 64 max_pages], starts as if within [0, tokens].
+ *   shorter  lens[i] may be made smaller, as after drafted tokens that were refused: to a length within the page that is open, or to whole pages (a multiple of 64).  Not to
+ *            one inside a full page: its tokens are held as codes alone, and the tail holds the next page's.  A program that may have to go back over a page's end keeps a copy
+ *            of the sequence's part of tails (kv_heads * 256 * dp bytes, see slicer_kv_sizes, from i times as many on) from before the append, puts it back, and appends
+ *            the tokens that stay once more.
  *   batches  a call's new tokens (queries) of sequence i are rows starts[i] .. starts[i + 1] - 1 of [tokens][heads][head_dim] tensors (device array, seqs + 1
  *            entries); a sequence may have none.  Rows outside every sequence are left as they were.  lens[i] counts the sequence's tokens with the call's new ones.
  *            max_new: no sequence has more new tokens (of a longer one, slicer_kv_attend leaves the queries behind them out).

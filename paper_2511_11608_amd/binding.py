@@ -355,7 +355,8 @@ def slicer_profile_events(start_event, stop_event) -> None:
 
 
 class KvCache:
-    """The cache's buffers (see slicer_kv in include/slicer.h): page_table and lens are the program's to keep."""
+    """The cache's buffers (see slicer_kv in include/slicer.h): page_table and lens are the program's to keep.  A length may be taken back within the open page
+    or to whole pages; over a page's end only with a copy of tails.view(seqs, -1)[i] from before the append, put back before the tokens that stay are appended again."""
 
     def __init__(self, pages, scales, tails, page_table, lens, seqs, kv_heads, head_dim, n_pages, max_pages):
         self.pages, self.scales, self.tails, self.page_table, self.lens = pages, scales, tails, page_table, lens
