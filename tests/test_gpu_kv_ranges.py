@@ -165,3 +165,58 @@ def test_the_largest_values_of_a_long_cache(max_len, n, dtype):
         # half a step, the probabilities' rounding, and sums in fp32, of the values and of the weights
         off = torch.finfo(p.dt).eps / 2 + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -21) + 2 * 70064 * 2.0 ** -24
         assert (np.abs(out.double().cpu().numpy() / 2.0 ** 95 - 1.0) <= off).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [8, 32, 64, 96, 128, 160, 192, 224, 256])
+def test_prompts_outside_the_pipeline_at_every_head_size(dim, dtype):
+    """Steep scores and value scales far apart at once, whole pages and a tail, pages shared out and not."""
+    torch = _torch()
+    p = Pair(1, 1, dim, 8, dtype, seed=dim)
+    total = 7 * PAGE + 9
+    rng = np.random.default_rng(dim)
+    k = whole_keys(rng.integers(-120, 121, total), dim, p.dt)
+    v = p.rand(total, 1).float().clamp(-4.0, 4.0)
+    for i, e in enumerate((0, 70, -70, 3, 0, 40, 0)):
+        v[i * PAGE: i * PAGE + PAGE] *= 2.0 ** e
+    v = v.to(p.dt)
+    n = 100
+    p.append([total - n], k[: total - n], v[: total - n])
+    p.append([n], k[total - n:], v[total - n:])
+    q = torch.zeros(n, 2, dim)
+    q[:, 0, 0], q[:, 1, 0] = 2.0 ** 24, -(2.0 ** 16)
+    q = q.to(p.dt)
+    for max_len in (None, 0):
+        mass = torch.zeros(1, 1, 8, device="cuda")
+        out, lse = p.attend([n], q.cuda(), 0.125, mass=mass, max_len=max_len)
+        check_exact_scores(p, [n], q, 0.125, out, lse, mass)
+
+
+def test_steep_tiles_leave_the_others_as_they_are():
+    """More row tiles than workgroups that keep weights: a workgroup goes from steep tiles to ordinary ones.  Sequences of ordinary scores have the same bits whatever
+    the others' scores are, and steep ones are right."""
+    torch = _torch()
+    seqs, G, R, D, n = 44, 3, 2, 16, 260
+    got = []
+    for steep in (False, True):
+        p = Pair(seqs, G, D, 6, "bf16", seed=2)
+        k, v, q = p.rand(seqs * n, G), p.rand(seqs * n, G), p.rand(seqs * n, G * R)
+        codes = np.random.default_rng(1).integers(-120, 121, n)
+        for b in range(0, seqs, 3):                         # one sequence of three
+            if steep:
+                k[b * n: b * n + n] = whole_keys(codes, D, p.dt)
+                q[b * n: b * n + n] = 0.0
+                q[b * n: b * n + n, :, 0] = 2.0 ** 26
+        p.append([n] * seqs, k, v)
+        mass = torch.zeros(seqs, G, 6, device="cuda")
+        out, lse = p.attend([n] * seqs, q.cuda(), 0.125, mass=mass)
+        got.append((out.view(seqs, n, G * R, D), lse.view(seqs, n, G * R), mass))
+        if steep:
+            for b in (0, 21, 42):
+                one, refs = slice(b * n, b * n + n), p.ref
+                p.ref = [refs[b]]
+                check_exact_scores(p, [n], q[one], 0.125, out[one], lse[one], mass[b: b + 1])
+                p.ref = refs
+    ordinary = [b for b in range(seqs) if b % 3]
+    assert all(torch.equal(a[ordinary], c[ordinary]) for a, c in zip(*got))
+    assert not torch.equal(got[0][0][0], got[1][0][0])
