@@ -380,6 +380,8 @@ int slicer_kv_read(const slicer_kv* kv, void* k, void* v, slicer_dtype dt, int64
  * recent_pages and the heaviest of the others stay, keep_pages in all.  A page's weight is the sum of mass over the kv heads, in fp64; equal weights: the
  * lower place stays (the rule of slicer_encode's top-K); NaN counts as largest.  Later pages move up in page_table and mass, the page that is not full and entries behind it too;
  * no codes move, and slots left over hold -1 and 0.  A later query sees the tokens that are left as its predecessors.
+ * lens then counts the tokens that are left: the place of a later token in its text (for rotary angles) is the program's own count.  freed names the sequence's entries
+ * as they stood: a page that other sequences share is theirs still.
  *   mass          [seqs][kv_heads][max_pages]
  *   page_table_out, lens_out, mass_out   as kv->page_table, kv->lens and mass, or those very arrays (no other overlap)
  *   freed         [seqs][max_pages]: the dropped pages in their order, then -1; n_freed [seqs]: how many

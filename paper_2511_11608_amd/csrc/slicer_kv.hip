@@ -92,9 +92,10 @@ AttendPlan plan_attend(const slicer_kv* kv, int heads, int64_t tokens, int max_n
     // leave more starts and more parts to join.  us for the append and the attention of a step, at most 256 workgroups and at least 512: 20 x 2000..2100 tokens, 8 heads of 256,
     // fp32 74 and 105; 40 x 2000..2100, 8 of 160 70 and 81; 24 x 3000..5000, 8 of 64 29 and 32; 1 x 30000, 8 of 128 24 and 27; 2 x 262016 195 and 195.  At most 128: 2 x 262016 230.
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (pages + 3) / 4));
-    // Unsplit sequences that leave three eighths of their last round of CUs empty are split in three where a wavefront still has eight pages of each share: 17 x 9000..12000 tokens,
-    // 8 heads of 128 90 us, unsplit 101, 33 x 9000..12000 160 and 181, fp32 33 x 4600..6200, 8 of 256 193 and 240; shorter ones lose (33 x 2250..3000 63 and 60), and so do
-    // fuller rounds (24 x 9000..12000 127 and 115).
+    // Unsplit sequences that leave at least three eighths of the CUs of their one or two rounds empty (129 to 160 and 257 to 320 tiles; from three rounds on the last one's empty CUs are too
+    // small a part for the rule, and nothing was measured there) are split in three where a wavefront still has eight pages of each share: 17 x 9000..12000 tokens, 8 heads of 128
+    // 90 us, unsplit 101, 33 x 9000..12000 160 and 181, fp32 33 x 4600..6200, 8 of 256 193 and 240; shorter ones lose (33 x 2250..3000 63 and 60), and so do fuller rounds
+    // (24 x 9000..12000 127 and 115).
     if (tiles > 128 && tiles * 8 <= (tiles + 255) / 256 * 256 * 5 && pages >= 96) p.splits = 3;
     p.launch.row_blocks = p.splits > 1 ? p.rows_pad : 0;
     p.launch.page_blocks = p.rows_pad && mass && (p.splits > 1 || p.rows_pad > 16 || kv->max_pages > kMassPages) ? (int)((pages + 255) / 256) : 0;

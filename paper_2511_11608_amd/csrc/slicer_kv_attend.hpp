@@ -2,8 +2,9 @@
 //
 // Codes enter the matrix products as they are, exact in bf16 (keys) and fp16 (values); a page's two scales are factors of its scores and of its
 // probabilities.  What a product rounds is therefore the queries (bf16 queries are exact, fp32 ones are split into three bf16 numbers) and the probabilities:
-// times 2^13 they are held in fp16 (11 bits, down to 2^-27 of the largest; fp32 outputs take a second fp16 number for the rest).  bf16
-// probabilities would have added as much error as the output's own rounding.  Scores, maxima, sums and outputs are fp32 throughout.
+// times 2^13 they are held in fp16 (11 bits, down to 2^-27 of the largest; fp32 outputs take a second fp16 number for the rest), in prompts times 2^8 and the ratio of two
+// value scales, 2^-6 to 2 (where the ratio is smallest: 11 bits down to 2^-16 of the largest, steps of 2^-26 below).  bf16 probabilities would have added as much error as the
+// output's own rounding.  Scores, maxima, sums (of the probabilities before that rounding) and outputs are fp32 throughout.
 // The tail's values are bf16 as they came and would not fit fp16: there the probabilities are split into bf16 numbers.
 #pragma once
 
@@ -535,11 +536,11 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttendArgs a, int row_bl
 // page ahead, turned into bf16 and fp16 operands once for all four and read from LDS as the lanes want them.  S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16
 // products, a lane has the scores of one row.  Bound by the matrix units, the exponentials and LDS reads, in about equal parts.
 // What was measured on 8 x 2048 queries, 32 heads over 8 of 128 (275 GFLOP), with the append: the pipeline of one wavefront, product by product with the vector
-// instructions that run beside it, 390 us (690 TFLOP/s in the kernel, where a large matrix product reaches 1390), a page after the other 444.  With 64 rows a wavefront (half of the LDS reads, one wavefront a SIMD) 568: two
-// wavefronts hide each other's waits better than one hides its own.  A page takes a wavefront 1.33 us alone on its SIMD, two of them 2.2;
-// in the whole kernel vector instructions are issued 57 % of the time, the matrix units work 35 %, LDS 31 %.
-
-
+// instructions that run beside it, 371 us (the kernel alone 354 at best, 780 TFLOP/s, where a large matrix product reaches 1390); when it came in, 390 against 444 for a page after the other
+// and 568 with 64 rows a wavefront (half of the LDS reads, one wavefront a SIMD): two wavefronts hide each other's waits better than one hides its own.  A page takes a wavefront 1.33 us
+// alone on its SIMD, two of them 2.2; in the whole kernel vector instructions are issued 57 % of the time, the matrix units work 36 %, LDS 32 %.
+// Scores and value scales that no model has (kSteep, page_scales) are outside what the pipeline can hold; a tile that meets them is done again, page after page.  With every tile
+// done so, the same shape takes 697 us.
 
 constexpr int kTileRows = 128;
 
@@ -615,7 +616,7 @@ __device__ inline float other_half(float x, float* mine)             // the valu
     return __uint_as_float(r[1]);
 }
 
-// `row_tiles` of 128 CT rows a head; workgroups that keep weights of a tile's rows by page on the way (a.mass) have a part of row_w each.
+// `row_tiles` of 128 rows a head; workgroups that keep weights of a tile's rows by page on the way (a.mass) have a part of row_w each.
 template <int DT, int DP>
 __global__ __launch_bounds__(256, DP * (DT == 1 ? 1 : 2) <= 128 ? 2 : 1) void kv_prompt_kernel(KvAttendArgs a, int row_tiles)
 {
