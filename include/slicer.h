@@ -321,7 +321,7 @@ int slicer_stream_words(const void* meta, uint64_t* words, void* hip_stream);
  * dt is the type of k, v, q and out; softmax, sums and weights are fp32.  All calls but slicer_kv_sizes and slicer_kv_attend_sizes, which are host
  * computations, are asynchronous on hip_stream, allocate nothing and can be captured into a HIP graph.  Calls that share a workspace, or of
  * which one writes what another reads, must be ordered by the caller; others may overlap.
- * Errors: SLICER_EINVAL for null pointers, seqs, heads, max_pages or n_pages < 1 (max_pages > 2^24, n_pages >= 2^31, seqs * kv_heads >= 2^22),
+ * Errors: SLICER_EINVAL for null pointers, seqs, heads, max_pages or n_pages < 1 (max_pages > 2^24, n_pages >= 2^31, seqs * kv_heads >= 2^22, pages of more than 2^62 bytes),
  * head_dim no multiple of 8 in 8..256, max_new < 1 with tokens > 0, tokens outside [0, 2^31), buffers off a 16-byte boundary, launches of 2^32 threads and more,
  * and what the calls name; SLICER_EUNSUPPORTED for an unknown dtype.
  */

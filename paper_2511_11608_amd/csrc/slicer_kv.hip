@@ -21,6 +21,7 @@ int check_kv(const slicer_kv* kv)
     if (kv->n_pages < 1 || kv->n_pages >= (int64_t)1 << 31) return SLICER_EINVAL;
     if ((int64_t)kv->seqs * kv->kv_heads >= (int64_t)1 << 22) return SLICER_EINVAL;
     if (kv->head_dim < 8 || kv->head_dim > 256 || kv->head_dim % 8) return SLICER_EINVAL;
+    if (kv->n_pages > ((int64_t)1 << 62) / ((int64_t)kv->kv_heads * (2 * kPage * round32(kv->head_dim)))) return SLICER_EINVAL;       // bytes of the pages
     return SLICER_OK;
 }
 

@@ -1,4 +1,6 @@
 """slicer_kv_*, calls that need no GPU: refusals of scales that fp32 does not hold, workspace sizes of calls made at the same time."""
+import ctypes as C
+
 import pytest
 
 from tests.test_kv_cpu import attend, handle, lib  # noqa: F401 (a fixture)
@@ -41,3 +43,13 @@ def test_workspace_sizes_of_two_calls_at_once(lib):  # noqa: F811
         assert Turn.other is None
     # and of another handle of the same cache
     assert kv.workspace_bytes(handle(seqs=200), *large) > want[1] and kv.workspace_bytes(c, *large) == want[1]
+
+
+def test_caches_of_more_bytes_than_a_size_holds_are_refused(lib):  # noqa: F811
+    n = C.c_size_t(7)
+    for kw in (dict(n_pages=(1 << 31) - 1, seqs=1, kv_heads=1 << 20, head_dim=256), dict(n_pages=1 << 30, seqs=1, kv_heads=1 << 21, head_dim=128)):
+        kv = handle(**kw)
+        assert lib.slicer_kv_sizes(C.byref(kv), C.byref(n), None, None) == -1 and n.value == 7
+        assert attend(lib, kv, heads=kv.kv_heads) == -1
+    kv = handle(n_pages=1 << 30, seqs=1, kv_heads=1 << 16, head_dim=128)
+    assert lib.slicer_kv_sizes(C.byref(kv), C.byref(n), None, None) == 0 and n.value == 1 << 60
