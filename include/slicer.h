@@ -359,7 +359,8 @@ int slicer_kv_append(const slicer_kv* kv, const void* k, const void* v, slicer_d
  *   mass       [seqs][kv_heads][max_pages] fp32 or NULL: mass = mass_decay * mass + the sum of the probabilities that the page's tokens got from the
  *              call's queries in the kv head's query heads, for the pages that hold tokens of sequences with new ones; others stay.  mass_decay in [0, 1]; with 0
  *              the old contents are not read.
- *   workspace  slicer_kv_attend_sizes bytes (with_mass: for calls with mass; enough for those without), 256-byte aligned; contents undefined before and after
+ *   workspace  slicer_kv_attend_sizes bytes (with_mass: for calls with mass; enough for those without), 256-byte aligned; contents undefined before and after; may
+ *              be NULL where that is 0
  *   max_len    what lens are expected to stay within; it decides how the work is split, never the result's validity
  * The result is a function of the arguments alone: nothing is summed in an order that changes from call to call.
  * Errors: SLICER_EINVAL for heads no multiple of kv_heads, scale (times log2(e)) not finite in fp32, mass_decay outside [0, 1], max_len < 0.

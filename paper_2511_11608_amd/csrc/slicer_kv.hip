@@ -183,8 +183,9 @@ int slicer_kv_attend(const slicer_kv* kv, const void* q, slicer_dtype dt, int he
     const float scale2 = (float)(std::fabs(scale) * 1.44269504088896340736);           // of scores that are exponents of 2
     if (heads < 1 || heads % kv->kv_heads || !std::isfinite(scale2) || !(mass_decay >= 0.0 && mass_decay <= 1.0) || max_len < 0) return SLICER_EINVAL;
     if (tokens == 0) return SLICER_OK;
-    if (!q || !out || !workspace || (((uintptr_t)out | (uintptr_t)workspace) & 15)) return SLICER_EINVAL;
+    if (!q || !out || (((uintptr_t)out | (uintptr_t)workspace) & 15)) return SLICER_EINVAL;
     const AttendPlan p = plan_attend(kv, heads, tokens, max_new, max_len, mass != nullptr);
+    if (p.total && !workspace) return SLICER_EINVAL;
     const int64_t pairs = (int64_t)kv->seqs * kv->kv_heads;
     for (int64_t n : {(int64_t)p.launch.split_tiles * p.splits, (int64_t)p.launch.row_blocks + p.launch.page_blocks, (int64_t)p.launch.prompt_tiles * (p.prompt_splits > 1 ? kTileRows : 1), (int64_t)p.launch.mass_blocks})
         if (pairs * n >= kMaxGroups) return SLICER_EINVAL;        // more workgroups than a launch can have

@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 from tests.test_kv_cpu import attend, handle, lib  # noqa: F401 (a fixture)
 
@@ -53,3 +54,14 @@ def test_caches_of_more_bytes_than_a_size_holds_are_refused(lib):  # noqa: F811
         assert attend(lib, kv, heads=kv.kv_heads) == -1
     kv = handle(n_pages=1 << 30, seqs=1, kv_heads=1 << 16, head_dim=128)
     assert lib.slicer_kv_sizes(C.byref(kv), C.byref(n), None, None) == 0 and n.value == 1 << 60
+
+
+def test_a_workspace_of_no_bytes_may_be_null(lib):  # noqa: F811
+    """Prompts of the same length without weights, more than the chip has places for, need none; whether they can be launched is another matter here."""
+    kv, n = handle(seqs=64, kv_heads=8, max_pages=32), C.c_size_t(7)
+    assert lib.slicer_kv_attend_sizes(C.byref(kv), 32, 64 * 512, 512, 512, 0, C.byref(n)) == 0 and n.value == 0
+    assert lib.slicer_kv_attend_sizes(C.byref(kv), 32, 64 * 512, 512, 512, 1, C.byref(n)) == 0 and n.value > 0
+    call = dict(heads=32, tokens=64 * 512, max_new=512, max_len=512, ws=None)
+    assert attend(lib, kv, mass=256, **call) == -1
+    if not torch.cuda.is_available():                       # (the handle's pointers lead nowhere)
+        assert attend(lib, kv, **call) == -3
